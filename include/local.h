@@ -403,6 +403,44 @@ local_status_t local_paged_attn_decode_noalloc(
     uint16_t* out, float* lse, void* stream);
 
 /*
+ * local_paged_attn_decode_weighted — local_paged_attn_decode that also adds up
+ * how much attention weight each block of a request receives (§2.2 "KV
+ * cache"; the use of cached state that decides what is kept). With w the
+ * softmax weights of the definition above and owned blocks j < nb_b:
+ *
+ *   weight_out[b,j] = weight_decay * weight_in[b,j]
+ *                     + sum over query heads h and positions pi in S with
+ *                       pi/16 = j of w[b,h,pi]
+ *   weight_out[b,j] = 0 for nb_b <= j < max_blocks
+ *
+ *  A stale block receives no weight; a row without any valid key gives none.
+ *  Calls of several layers that share one block table may add to one array,
+ *  one after the other.
+ *   weight_in     [B][max_blocks] float32, or NULL (zeros)
+ *   weight_decay  in [0, 1]
+ *   weight_out    [B][max_blocks] float32; may be weight_in itself (in place),
+ *                 must not overlap it otherwise
+ *  All other arguments, the results in out/lse and the appended slots: as
+ *  local_paged_attn_decode. Weights are float32 sums in a fixed order.
+ *  Errors as local_paged_attn_decode; LOCAL_ERR_NULL for a NULL weight_out with
+ *  B > 0, LOCAL_ERR_UNSUPPORTED for another weight_decay or Hq > 8192.
+ *  Workspace: as local_paged_attn_decode (the size asked for), rounded up to
+ *  256 bytes, then 4 bytes for each (request, block of the table, query head).
+ */
+local_status_t local_paged_attn_decode_weighted(
+    const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+    const uint16_t* k_new, const uint16_t* v_new,
+    uint16_t* k_cache, uint16_t* v_cache,
+    int64_t num_blocks, int32_t block_size,
+    const int32_t* block_table, int32_t max_blocks,
+    const int32_t* ctx_lens,
+    const int32_t* block_version, const int32_t* req_version,
+    float sm_scale,
+    uint16_t* out, float* lse,
+    const float* weight_in, float weight_decay, float* weight_out,
+    void* ws, size_t* ws_bytes, void* stream);
+
+/*
  * local_paged_attn_prefill — a chunk of new tokens per request is appended to
  * the paged cache and attends causally over the cached prefix plus the chunk,
  * with the per-block version mask (§4.1 chunked prefill; §5.3 stale-coverage
@@ -505,6 +543,170 @@ local_status_t local_kv_pool_export(
     const uint16_t* k_cache, const uint16_t* v_cache,
     int64_t num_blocks, int32_t Hkv, int32_t D, int32_t block_size,
     uint16_t* k_tok, uint16_t* v_tok, void* stream);
+
+/*
+ * 4-bit KV block pool (one attention layer)
+ * -----------------------------------------
+ *  The same blocks in 4.25 bits a value (§2.2 "KV cache": the state that bounds
+ *  how many contexts one GPU holds). K and V of a (token, KV head) are rounded
+ *  in groups of 32 neighbouring dims:
+ *    amax = max |x| over the group; E the least integer with amax <= 6 * 2^E,
+ *    at least -125 and at most 125 (amax = 0: -125)
+ *    value = sign * m * 2^E with m the nearest of {0, 0.5, 1, 1.5, 2, 3, 4, 6}
+ *    to |x| / 2^E, ties to the even index, beyond 6 to 6
+ *  A group that holds an infinity or a NaN stands for NaN as a whole. What a
+ *  group stands for is exact in bf16.
+ *   kv4  [num_blocks][Hkv][17*D] uint8, 16-byte aligned. A (block, KV head)
+ *        tile holds, in bytes (code c of a value: its index of m in the low
+ *        three bits, its sign in the fourth; of two codes in a byte the even
+ *        dim's is the low half):
+ *     code of K(slot, d)   ((d / (D/4))*16 + slot)*(D/8) + (d % (D/4))/2
+ *     code of V(slot, d)   8*D + (((slot/4)*16 + d / (D/16))*4 + slot%4)*(D/32)
+ *                          + (d % (D/16))/2
+ *     scale of K(slot, d)  16*D + (d/32)*16 + slot
+ *     scale of V(slot, d)  16*D + D/2 + ((slot/4)*(D/32) + d/32)*4 + slot%4
+ *        A scale is the byte E + 127, or 255 (codes 0) for a group that stands
+ *        for NaN.
+ *  Block ids, slots, tables and tags are those of the bf16 pool.
+ *
+ * local_kv4_pool_import / local_kv4_pool_export — blocks of the bf16 pool into
+ * the 4-bit pool and back.
+ *
+ *   k_cache, v_cache  bf16 pool of num_blocks blocks
+ *   kv4               4-bit pool of num_blocks blocks
+ *   block_ids         [n_ids] int32: the blocks to convert; n_ids = -1 for all
+ *                     (block_ids is then ignored). Each keeps its id; blocks not
+ *                     listed are not touched; an id outside [0, num_blocks) is
+ *                     skipped, one listed twice is converted twice to the
+ *                     same result.
+ *
+ *  import reads k_cache and v_cache and writes kv4; export reads kv4 and writes
+ *  k_cache and v_cache (exactly). Sizes: num_blocks >= 0, n_ids >= -1 (nothing to
+ *  convert: nothing is launched and the pointers may be NULL), Hkv >= 1, D in
+ *  {64,128}, block_size == 16. Errors: LOCAL_ERR_NULL for a NULL pool or list,
+ *  LOCAL_ERR_SHAPE for other sizes below 0, Hkv < 1 or pools that overlap,
+ *  LOCAL_ERR_UNSUPPORTED for another D or block_size, or a pool that does not
+ *  start on 16 bytes. No workspace.
+ */
+local_status_t local_kv4_pool_import(
+    const uint16_t* k_cache, const uint16_t* v_cache,
+    int64_t num_blocks, int32_t Hkv, int32_t D, int32_t block_size,
+    const int32_t* block_ids, int64_t n_ids,
+    uint8_t* kv4, void* stream);
+
+local_status_t local_kv4_pool_export(
+    const uint8_t* kv4,
+    int64_t num_blocks, int32_t Hkv, int32_t D, int32_t block_size,
+    const int32_t* block_ids, int64_t n_ids,
+    uint16_t* k_cache, uint16_t* v_cache, void* stream);
+
+/*
+ * local_paged_attn_decode_kv4 — decode attention over the 4-bit pool: as
+ * local_paged_attn_decode (and, with weight_out, as
+ * local_paged_attn_decode_weighted), where K and V are the values that the
+ * pool stands for. k_new/v_new are rounded as above, written at position
+ * ctx_lens[b]-1, and attended to as written.
+ *
+ *   kv4          4-bit pool of num_blocks blocks; written only at the appended
+ *                slots
+ *   weight_in, weight_decay, weight_out   as local_paged_attn_decode_weighted;
+ *                weight_out NULL: no weights (then weight_in must be NULL)
+ *   other arguments as in decode.
+ *
+ *  A group that stands for NaN makes the outputs NaN that it enters (a stale
+ *  block's, or a slot past ctx_lens[b], enters none).
+ *  Sizes and errors as local_paged_attn_decode; q, k_new, v_new, kv4, out and ws
+ *  must start on 16 bytes (LOCAL_ERR_UNSUPPORTED otherwise). Workspace: the size
+ *  asked for.
+ */
+local_status_t local_paged_attn_decode_kv4(
+    const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+    const uint16_t* k_new, const uint16_t* v_new,
+    uint8_t* kv4,
+    int64_t num_blocks, int32_t block_size,
+    const int32_t* block_table, int32_t max_blocks,
+    const int32_t* ctx_lens,
+    const int32_t* block_version, const int32_t* req_version,
+    float sm_scale,
+    uint16_t* out, float* lse,
+    const float* weight_in, float weight_decay, float* weight_out,
+    void* ws, size_t* ws_bytes, void* stream);
+
+/*
+ * local_paged_attn_prefill_kv4 — chunked prefill over the 4-bit pool: as
+ * local_paged_attn_prefill, where K and V are the values that the pool stands
+ * for. The chunk's k_new/v_new are rounded as above, written first, and
+ * attended to as written.
+ *
+ *   kv4          4-bit pool of num_blocks blocks; written only at the chunks'
+ *                slots
+ *   other arguments as in prefill (a request whose range of rows is not inside
+ *   [0, T] is skipped whole; ranges must not overlap).
+ *
+ *  A row's result depends only on the keys it sees: a later token of its chunk
+ *  whose values are not finite does not reach it.
+ *  Sizes and errors as local_paged_attn_prefill, T * Hq / Hkv below 2^30; q, k_new,
+ *  v_new, kv4, out and ws must start on 16 bytes (LOCAL_ERR_UNSUPPORTED
+ *  otherwise). Workspace: the size asked for, which may be 0 (ws must then
+ *  still not be NULL, or the call is taken for the query).
+ */
+local_status_t local_paged_attn_prefill_kv4(
+    const uint16_t* q, const int32_t* q_indptr, int32_t B, int64_t T,
+    int32_t Hq, int32_t Hkv, int32_t D,
+    const uint16_t* k_new, const uint16_t* v_new,
+    uint8_t* kv4,
+    int64_t num_blocks, int32_t block_size,
+    const int32_t* block_table, int32_t max_blocks,
+    const int32_t* ctx_lens,
+    const int32_t* block_version, const int32_t* req_version,
+    float sm_scale,
+    uint16_t* out, float* lse,
+    void* ws, size_t* ws_bytes, void* stream);
+
+/*
+ * local_kv_evict — cut requests' contexts down to a budget of blocks by the
+ * attention weight that each block has received (§5.4 releases cached state
+ * coldest first; here within one request, by the weights of
+ * local_paged_attn_decode_weighted or _kv4).
+ *
+ *  Request b owns nb_b blocks as above. Its first sink_blocks and last
+ *  recent_blocks blocks are protected; it keeps
+ *    n_b = min(nb_b, max(keep_blocks[b], number of protected blocks))
+ *  blocks: the protected ones and, of the others, those of the largest
+ *  block_weight (a weight that is not above 0, or NaN, counts as 0), equal
+ *  weights by ascending j, stale blocks after all that are not. The kept blocks
+ *  move up in order:
+ *    table_out[b, 0..n_b)    ids of the kept blocks in ascending j, then -1
+ *    weight_out[b, 0..n_b)   their weights, then 0
+ *    ctx_out[b]              ctx_lens[b] - 16 * (nb_b - n_b)
+ *    evicted[b, 0..nb_b-n_b) ids of the evicted blocks in ascending j, then -1
+ *    n_evicted[b]            nb_b - n_b
+ *  No KV is moved: the pool's blocks stay as they are, and the caller returns
+ *  the evicted ids to its allocator (a block that another request's table
+ *  holds too is the caller's to count).
+ *
+ *   block_table  [B][max_blocks] int32;  ctx_lens [B] int32 in [0, 16*max_blocks]
+ *   block_weight [B][max_blocks] float32
+ *   keep_blocks  [B] int32
+ *   block_version [num_blocks], req_version [B] int32
+ *   table_out [B][max_blocks] int32, ctx_out [B] int32, weight_out
+ *                [B][max_blocks] float32: each may be the input itself (in
+ *                place), and must not overlap it otherwise
+ *   evicted      [B][max_blocks] int32, n_evicted [B] int32; must not overlap an
+ *                input
+ *  Sizes: B >= 0, max_blocks >= 1, num_blocks >= 1, sink_blocks >= 0,
+ *  recent_blocks >= 1 (the last block, which the next token goes into, is always
+ *  kept), block_size == 16. The result is exact and deterministic. No workspace.
+ */
+local_status_t local_kv_evict(
+    const int32_t* block_table, int32_t B, int32_t max_blocks,
+    const int32_t* ctx_lens, int32_t block_size,
+    const float* block_weight, const int32_t* keep_blocks,
+    int32_t sink_blocks, int32_t recent_blocks,
+    const int32_t* block_version, int64_t num_blocks,
+    const int32_t* req_version,
+    int32_t* table_out, int32_t* ctx_out, float* weight_out,
+    int32_t* evicted, int32_t* n_evicted, void* stream);
 
 #ifdef __cplusplus
 }

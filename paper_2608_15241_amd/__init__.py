@@ -16,4 +16,9 @@ from .binding import (BLOCK_SIZE, EXPORTS, LIB_PATH, Call, KVManager, LocalError
                       prepare_lora_grad, prepare_lora_grad_grouped, prepare_lora_grad_input,
                       prepare_lora_linear,
                       prepare_lora_linear_grouped,
-                      prepare_paged_attn_decode, prepare_paged_attn_prefill)
+                      prepare_paged_attn_decode, prepare_paged_attn_prefill,
+                      local_kv4_pool_export, local_kv4_pool_import, local_kv_evict,
+                      local_paged_attn_decode_kv4, local_paged_attn_decode_weighted,
+                      local_paged_attn_prefill_kv4, prepare_kv4_pool_export,
+                      prepare_kv4_pool_import, prepare_kv_evict, prepare_paged_attn_decode_kv4,
+                      prepare_paged_attn_decode_weighted, prepare_paged_attn_prefill_kv4)

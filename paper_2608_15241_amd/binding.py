@@ -29,6 +29,8 @@ EXPORTS = ("local_last_error", "local_version", "local_lora_linear",
            "local_block_version_check", "local_lora_grad", "local_lora_grad_input",
            "local_lora_grad_grouped", "local_paged_attn_decode_noalloc",
            "local_paged_attn_decode_checked", "local_kv_pool_import", "local_kv_pool_export",
+           "local_paged_attn_decode_weighted", "local_kv4_pool_import", "local_kv4_pool_export",
+           "local_paged_attn_decode_kv4", "local_paged_attn_prefill_kv4", "local_kv_evict",
            # host-side KV manager (local_kv.h)
            "local_kvm_default_params", "local_kvm_create", "local_kvm_destroy",
            "local_kvm_tags", "local_kvm_set_committed", "local_kvm_stage", "local_kvm_publish",
@@ -106,6 +108,23 @@ def load_library(path: str = LIB_PATH):
         f = getattr(lib, name)
         f.restype = ctypes.c_int
         f.argtypes = [P, P, i64, i32, i32, i32, P, P, P]
+    lib.local_paged_attn_decode_weighted.restype = ctypes.c_int
+    lib.local_paged_attn_decode_weighted.argtypes = [P, i32, i32, i32, i32, P, P, P, P, i64, i32,
+                                                     P, i32, P, P, P, f32, P, P, P, f32, P, P,
+                                                     SZ, P]
+    lib.local_kv4_pool_import.restype = ctypes.c_int
+    lib.local_kv4_pool_import.argtypes = [P, P, i64, i32, i32, i32, P, i64, P, P]
+    lib.local_kv4_pool_export.restype = ctypes.c_int
+    lib.local_kv4_pool_export.argtypes = [P, i64, i32, i32, i32, P, i64, P, P, P]
+    lib.local_paged_attn_decode_kv4.restype = ctypes.c_int
+    lib.local_paged_attn_decode_kv4.argtypes = [P, i32, i32, i32, i32, P, P, P, i64, i32, P, i32,
+                                                P, P, P, f32, P, P, P, f32, P, P, SZ, P]
+    lib.local_paged_attn_prefill_kv4.restype = ctypes.c_int
+    lib.local_paged_attn_prefill_kv4.argtypes = [P, P, i32, i64, i32, i32, i32, P, P, P, i64, i32,
+                                                 P, i32, P, P, P, f32, P, P, P, SZ, P]
+    lib.local_kv_evict.restype = ctypes.c_int
+    lib.local_kv_evict.argtypes = [P, i32, i32, P, i32, P, P, i32, i32, P, i64, P, P, P, P, P, P,
+                                   P]
     _declare_kvm(lib)
     _declare_sched(lib)
     _lib = lib
@@ -221,6 +240,23 @@ def _req(t: torch.Tensor, name: str, dtype, ndim: Optional[int] = None):
     return t
 
 
+def _one_device(*tensors) -> int:
+    """The index of the device that all of the tensors are on (None entries aside), which
+    must be the current one: the call goes to its current stream."""
+    devices = {t.device.index for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError("tensors on several devices: %s" % sorted(devices))
+    on = devices.pop()
+    _on_device(on)
+    return on
+
+
+def _on_device(on: Optional[int]):
+    if on is not None and torch.cuda.current_device() != on:
+        raise ValueError("the tensors are on device %d, the current one is %d"
+                         % (on, torch.cuda.current_device()))
+
+
 class Workspace:
     """A grow-only device byte buffer reused across calls on one stream."""
 
@@ -254,7 +290,7 @@ class Call:
     """
 
     def __init__(self, fn, args_before_ws, workspace: Optional[Workspace], device,
-                 keep=()):
+                 keep=(), on: Optional[int] = None):
         # The call holds raw device pointers: keep every tensor it points to
         # alive for as long as the call can run (including graph replays).
         self.keep = tuple(t for t in keep if t is not None)
@@ -265,8 +301,10 @@ class Call:
         self.fn = fn
         self.args = tuple(args_before_ws) + (_ptr(self.ws), ctypes.byref(self.ws_bytes))
         self.outputs = None
+        self.on = on  # where given, the device that has to be current at every call
 
     def __call__(self):
+        _on_device(self.on)
         _check(self.fn(*self.args, _stream()))
         return self.outputs
 
@@ -652,13 +690,15 @@ def local_paged_attn_decode_checked(*args, **kwargs):
 class NoWorkspaceCall:
     """A prepared C-ABI call of an entry point that takes no workspace."""
 
-    def __init__(self, fn, args, keep=()):
+    def __init__(self, fn, args, keep=(), on: Optional[int] = None):
         self.keep = tuple(t for t in keep if t is not None)
         self.fn = fn
         self.args = tuple(args)
         self.outputs = None
+        self.on = on  # as in Call
 
     def __call__(self):
+        _on_device(self.on)
         _check(self.fn(*self.args, _stream()))
         return self.outputs
 
@@ -828,6 +868,257 @@ def local_kv_pool_export(k_cache, v_cache, D, k_tok=None, v_tok=None):
                                     _ptr(k_tok), _ptr(v_tok), _stream()))
     return k_tok, v_tok
 
+
+# ------------------------------------------------------------ block weights, 4-bit pool
+def _new_kv_checks(k_new, v_new, rows, Hkv, D):
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new must be given together")
+    if k_new is not None:
+        _req(k_new, "k_new", torch.bfloat16, 3)
+        _req(v_new, "v_new", torch.bfloat16, 3)
+        if tuple(k_new.shape) != (rows, Hkv, D) or tuple(v_new.shape) != (rows, Hkv, D):
+            raise ValueError("k_new/v_new must be [%d, %d, %d]" % (rows, Hkv, D))
+
+
+def _weight_checks(weight_in, weight_out, block_table):
+    for t, n in ((weight_in, "weight_in"), (weight_out, "weight_out")):
+        if t is not None:
+            _req(t, n, torch.float32, 2)
+            if t.shape != block_table.shape:
+                raise ValueError("%s must be %s like the block table, got %s"
+                                 % (n, tuple(block_table.shape), tuple(t.shape)))
+
+
+def prepare_paged_attn_decode_weighted(q, k_cache, v_cache, block_table, ctx_lens, block_version,
+                                       req_version, sm_scale: float, k_new=None, v_new=None,
+                                       Hkv: Optional[int] = None, out=None, lse=None,
+                                       weight_in=None, weight_out=None,
+                                       weight_decay: float = 1.0,
+                                       workspace: Optional[Workspace] = None) -> Call:
+    """Prepared decode attention that also adds up the weight of each block; the call
+    returns (out, lse, weight_out). weight_out may be weight_in (in place); without one
+    a new array is made at preparation."""
+    lib = load_library()
+    _req(q, "q", torch.bfloat16, 3)
+    B, Hq, D = q.shape
+    if Hkv is None:
+        if k_new is None:
+            raise ValueError("Hkv is required when k_new is not given")
+        Hkv = k_new.shape[1]
+    num_blocks = _pool_checks(k_cache, v_cache, Hkv, D)
+    _meta_checks(block_table, ctx_lens, block_version, req_version, B, num_blocks)
+    _new_kv_checks(k_new, v_new, B, Hkv, D)
+    out, lse = _attn_out_checks(out, lse, B, Hq, D, q.device)
+    if weight_out is None:
+        weight_out = torch.empty(block_table.shape, dtype=torch.float32, device=q.device)
+    _weight_checks(weight_in, weight_out, block_table)
+    keep = (q, k_new, v_new, k_cache, v_cache, block_table, ctx_lens, block_version, req_version,
+            out, lse, weight_in, weight_out)
+    on = _one_device(*keep)
+    args = [_ptr(q), B, Hq, Hkv, D, _ptr(k_new), _ptr(v_new), _ptr(k_cache), _ptr(v_cache),
+            num_blocks, BLOCK_SIZE, _ptr(block_table), block_table.shape[1], _ptr(ctx_lens),
+            _ptr(block_version), _ptr(req_version), float(sm_scale), _ptr(out), _ptr(lse),
+            _ptr(weight_in), float(weight_decay), _ptr(weight_out)]
+    c = Call(lib.local_paged_attn_decode_weighted, args, workspace, q.device, keep=keep, on=on)
+    c.outputs = (out, lse, weight_out)
+    return c
+
+
+def local_paged_attn_decode_weighted(*args, **kwargs):
+    """Decode attention plus the attention weight of each block (see include/local.h);
+    returns (out, lse, weight_out [B, max_blocks] float32)."""
+    return prepare_paged_attn_decode_weighted(*args, **kwargs)()
+
+
+def _kv4_checks(kv4, D=None):
+    """(num_blocks, Hkv, D) of a 4-bit pool [num_blocks, Hkv, 17*D] uint8."""
+    _req(kv4, "kv4", torch.uint8, 3)
+    nb, hkv, tile = kv4.shape
+    if tile % 17 or (D is not None and tile != 17 * D):
+        raise ValueError("kv4 must be [num_blocks, Hkv, 17*D%s], got %s"
+                         % ("" if D is None else "=%d" % (17 * D), tuple(kv4.shape)))
+    return nb, hkv, tile // 17
+
+
+def _block_ids(ids):
+    if ids is None:
+        return -1
+    _req(ids, "block_ids", torch.int32, 1)
+    return ids.shape[0]
+
+
+def _pool3_checks(k_cache, v_cache, nb, hkv, D):
+    for t, n in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _req(t, n, torch.bfloat16, 3)
+        if tuple(t.shape) != (nb, hkv, BLOCK_SIZE * D):
+            raise ValueError("%s must be [%d, %d, %d], got %s"
+                             % (n, nb, hkv, BLOCK_SIZE * D, tuple(t.shape)))
+
+
+def prepare_kv4_pool_import(k_cache, v_cache, kv4=None, block_ids=None) -> NoWorkspaceCall:
+    """Prepared conversion of blocks of the bf16 pool [num_blocks, Hkv, 16*D] into the
+    4-bit pool; the call returns kv4 (zeros where it was not given and no id names the
+    block)."""
+    lib = load_library()
+    _req(k_cache, "k_cache", torch.bfloat16, 3)
+    nb, hkv, bd = k_cache.shape
+    if bd % BLOCK_SIZE:
+        raise ValueError("k_cache must be [num_blocks, Hkv, 16*D], got %s"
+                         % (tuple(k_cache.shape),))
+    D = bd // BLOCK_SIZE
+    _pool3_checks(k_cache, v_cache, nb, hkv, D)
+    n = _block_ids(block_ids)
+    if kv4 is None:
+        make = torch.empty if block_ids is None else torch.zeros
+        kv4 = make((nb, hkv, 17 * D), dtype=torch.uint8, device=k_cache.device)
+    if _kv4_checks(kv4, D)[:2] != (nb, hkv):
+        raise ValueError("kv4 must have the bf16 pool's blocks and heads")
+    keep = (k_cache, v_cache, kv4, block_ids)
+    c = NoWorkspaceCall(lib.local_kv4_pool_import,
+                        (_ptr(k_cache), _ptr(v_cache), nb, hkv, D, BLOCK_SIZE, _ptr(block_ids), n,
+                         _ptr(kv4)), keep=keep, on=_one_device(*keep))
+    c.outputs = kv4
+    return c
+
+
+def local_kv4_pool_import(*args, **kwargs):
+    """Blocks of the bf16 pool into the 4-bit pool (see prepare_kv4_pool_import)."""
+    return prepare_kv4_pool_import(*args, **kwargs)()
+
+
+def prepare_kv4_pool_export(kv4, k_cache=None, v_cache=None, block_ids=None) -> NoWorkspaceCall:
+    """Prepared conversion of blocks of the 4-bit pool into the bf16 pool; the call returns
+    (k_cache, v_cache) (zeros where they were not given and no id names the block)."""
+    lib = load_library()
+    nb, hkv, D = _kv4_checks(kv4)
+    n = _block_ids(block_ids)
+    make = torch.empty if block_ids is None else torch.zeros
+    if k_cache is None:
+        k_cache = make((nb, hkv, BLOCK_SIZE * D), dtype=torch.bfloat16, device=kv4.device)
+    if v_cache is None:
+        v_cache = make((nb, hkv, BLOCK_SIZE * D), dtype=torch.bfloat16, device=kv4.device)
+    _pool3_checks(k_cache, v_cache, nb, hkv, D)
+    keep = (kv4, k_cache, v_cache, block_ids)
+    c = NoWorkspaceCall(lib.local_kv4_pool_export,
+                        (_ptr(kv4), nb, hkv, D, BLOCK_SIZE, _ptr(block_ids), n, _ptr(k_cache),
+                         _ptr(v_cache)), keep=keep, on=_one_device(*keep))
+    c.outputs = (k_cache, v_cache)
+    return c
+
+
+def local_kv4_pool_export(*args, **kwargs):
+    """Blocks of the 4-bit pool into the bf16 pool (see prepare_kv4_pool_export)."""
+    return prepare_kv4_pool_export(*args, **kwargs)()
+
+
+def prepare_paged_attn_decode_kv4(q, kv4, block_table, ctx_lens, block_version, req_version,
+                                  sm_scale: float, k_new=None, v_new=None, out=None, lse=None,
+                                  weight_in=None, weight_out=None, weight_decay: float = 1.0,
+                                  workspace: Optional[Workspace] = None) -> Call:
+    """Prepared decode attention over the 4-bit pool; the call returns (out, lse), and with
+    weight_in or weight_out (out, lse, weight_out)."""
+    lib = load_library()
+    _req(q, "q", torch.bfloat16, 3)
+    B, Hq, D = q.shape
+    num_blocks, Hkv, _ = _kv4_checks(kv4, D)
+    _meta_checks(block_table, ctx_lens, block_version, req_version, B, num_blocks)
+    _new_kv_checks(k_new, v_new, B, Hkv, D)
+    out, lse = _attn_out_checks(out, lse, B, Hq, D, q.device)
+    if weight_in is not None and weight_out is None:
+        weight_out = torch.empty_like(weight_in)
+    _weight_checks(weight_in, weight_out, block_table)
+    keep = (q, k_new, v_new, kv4, block_table, ctx_lens, block_version, req_version, out, lse,
+            weight_in, weight_out)
+    on = _one_device(*keep)
+    args = [_ptr(q), B, Hq, Hkv, D, _ptr(k_new), _ptr(v_new), _ptr(kv4), num_blocks, BLOCK_SIZE,
+            _ptr(block_table), block_table.shape[1], _ptr(ctx_lens), _ptr(block_version),
+            _ptr(req_version), float(sm_scale), _ptr(out), _ptr(lse), _ptr(weight_in),
+            float(weight_decay), _ptr(weight_out)]
+    c = Call(lib.local_paged_attn_decode_kv4, args, workspace, q.device, keep=keep, on=on)
+    c.outputs = (out, lse) if weight_out is None else (out, lse, weight_out)
+    return c
+
+
+def local_paged_attn_decode_kv4(*args, **kwargs):
+    """One query token per request over the 4-bit pool (see include/local.h)."""
+    return prepare_paged_attn_decode_kv4(*args, **kwargs)()
+
+
+def prepare_paged_attn_prefill_kv4(q, q_indptr, kv4, block_table, ctx_lens, block_version,
+                                   req_version, sm_scale: float, k_new=None, v_new=None, out=None,
+                                   lse=None, workspace: Optional[Workspace] = None) -> Call:
+    """Prepared chunked-prefill attention over the 4-bit pool; the call returns (out, lse)."""
+    lib = load_library()
+    _req(q, "q", torch.bfloat16, 3)
+    T, Hq, D = q.shape
+    _req(q_indptr, "q_indptr", torch.int32, 1)
+    B = q_indptr.shape[0] - 1
+    num_blocks, Hkv, _ = _kv4_checks(kv4, D)
+    _meta_checks(block_table, ctx_lens, block_version, req_version, B, num_blocks)
+    _new_kv_checks(k_new, v_new, T, Hkv, D)
+    out, lse = _attn_out_checks(out, lse, T, Hq, D, q.device)
+    keep = (q, q_indptr, k_new, v_new, kv4, block_table, ctx_lens, block_version, req_version,
+            out, lse)
+    on = _one_device(*keep)
+    args = [_ptr(q), _ptr(q_indptr), B, T, Hq, Hkv, D, _ptr(k_new), _ptr(v_new), _ptr(kv4),
+            num_blocks, BLOCK_SIZE, _ptr(block_table), block_table.shape[1], _ptr(ctx_lens),
+            _ptr(block_version), _ptr(req_version), float(sm_scale), _ptr(out), _ptr(lse)]
+    c = Call(lib.local_paged_attn_prefill_kv4, args, workspace, q.device, keep=keep, on=on)
+    c.outputs = (out, lse)
+    return c
+
+
+def local_paged_attn_prefill_kv4(*args, **kwargs):
+    """Chunked prefill over the 4-bit pool (see include/local.h)."""
+    return prepare_paged_attn_prefill_kv4(*args, **kwargs)()
+
+
+def prepare_kv_evict(block_table, ctx_lens, block_weight, keep_blocks, block_version, req_version,
+                     sink_blocks: int = 1, recent_blocks: int = 2, table_out=None, ctx_out=None,
+                     weight_out=None, evicted=None, n_evicted=None) -> NoWorkspaceCall:
+    """Prepared eviction of the blocks of least weight; the call returns (table_out, ctx_out,
+    weight_out, evicted, n_evicted). The first three may be the inputs (in place)."""
+    lib = load_library()
+    _req(block_table, "block_table", torch.int32, 2)
+    B, max_blocks = block_table.shape
+    _meta_checks(block_table, ctx_lens, block_version, req_version, B)
+    _req(block_weight, "block_weight", torch.float32, 2)
+    _req(keep_blocks, "keep_blocks", torch.int32, 1)
+    dev = block_table.device
+    new = torch.empty
+    table_out = new((B, max_blocks), dtype=torch.int32, device=dev) if table_out is None \
+        else _req(table_out, "table_out", torch.int32, 2)
+    ctx_out = new((B,), dtype=torch.int32, device=dev) if ctx_out is None \
+        else _req(ctx_out, "ctx_out", torch.int32, 1)
+    weight_out = new((B, max_blocks), dtype=torch.float32, device=dev) if weight_out is None \
+        else _req(weight_out, "weight_out", torch.float32, 2)
+    evicted = new((B, max_blocks), dtype=torch.int32, device=dev) if evicted is None \
+        else _req(evicted, "evicted", torch.int32, 2)
+    n_evicted = new((B,), dtype=torch.int32, device=dev) if n_evicted is None \
+        else _req(n_evicted, "n_evicted", torch.int32, 1)
+    for t, n in ((block_weight, "block_weight"), (table_out, "table_out"),
+                 (weight_out, "weight_out"), (evicted, "evicted")):
+        if tuple(t.shape) != (B, max_blocks):
+            raise ValueError("%s must be [%d, %d], got %s" % (n, B, max_blocks, tuple(t.shape)))
+    for t, n in ((keep_blocks, "keep_blocks"), (ctx_out, "ctx_out"), (n_evicted, "n_evicted")):
+        if t.shape[0] != B:
+            raise ValueError("%s must have B=%d entries, got %d" % (n, B, t.shape[0]))
+    keep = (block_table, ctx_lens, block_weight, keep_blocks, block_version, req_version,
+            table_out, ctx_out, weight_out, evicted, n_evicted)
+    on = _one_device(*keep)
+    args = [_ptr(block_table), B, max_blocks, _ptr(ctx_lens), BLOCK_SIZE, _ptr(block_weight),
+            _ptr(keep_blocks), int(sink_blocks), int(recent_blocks), _ptr(block_version),
+            block_version.numel(), _ptr(req_version), _ptr(table_out), _ptr(ctx_out),
+            _ptr(weight_out), _ptr(evicted), _ptr(n_evicted)]
+    c = NoWorkspaceCall(lib.local_kv_evict, args, keep=keep, on=on)
+    c.outputs = (table_out, ctx_out, weight_out, evicted, n_evicted)
+    return c
+
+
+def local_kv_evict(*args, **kwargs):
+    """Contexts down to a budget of blocks, by accumulated attention weight (see
+    include/local.h); returns (table_out, ctx_out, weight_out, evicted, n_evicted)."""
+    return prepare_kv_evict(*args, **kwargs)()
 
 # ------------------------------------------------------------ KV manager
 

@@ -35,197 +35,12 @@
 //  * The new token's K/V are written at position L-1 by the wave that owns
 //    that block, which also substitutes them for the cache slot it reads, so
 //    no other workgroup and no second launch is involved.
-#include <algorithm>
 #include <mutex>
 
-#include "common.hpp"
+#include "paged_attn_decode.hpp"
 
 namespace localk {
 namespace {
-
-// Blocks per partition, by the width of the block table: 32 up to 256 blocks,
-// 48 up to 512, 64 beyond (at most 64: one bit per lane in the stale masks).
-// Measured: the 32-layer decode with contexts up to 16K tokens (1024-block
-// tables) is 3.2% faster a step with 64 than with 32, the GQA decode with
-// 512-block tables 2% faster with 48, and the MHA decode with 256-block tables
-// fastest with 32 (fewer, longer partitions: less merge traffic and fewer
-// waves; shorter ones: more parallelism per request).
-//
-// A call with fewer than kFewUnits (KV head, request, partition) units leaves
-// compute units idle or unevenly loaded, and halves the partitions until it
-// has that many, down to 16 blocks and up to kMaxFine partitions a request
-// (whose merge is a serial pass). Measured, 8 KV heads of 4 query heads:
-// 5 requests of up to 15K tokens 55 us with 64 blocks and 36 with 32 (600 and
-// 1200 units); 8 of up to 4000 tokens 31 us with 32 and 21 with 16; one of
-// 16000 tokens (4 waves each) 22 us with 64, 17 with 32, 20 with 16 (62
-// partitions).
-constexpr int kFewUnits = 768;
-constexpr int kMaxFine = 32;
-
-int parts_of_table(int max_blocks, int pb) { return (max_blocks + pb - 1) / pb; }
-
-int longest_part_blocks(int max_blocks) {
-  return max_blocks <= 256 ? 32 : max_blocks <= 512 ? 48 : 64;
-}
-
-int part_blocks(int max_blocks, int64_t heads) {  // heads: B * Hkv
-  int pb = longest_part_blocks(max_blocks);
-  while (pb > 16 && heads * parts_of_table(max_blocks, pb) < kFewUnits) {
-    const int half = pb == 64 ? 32 : 16;
-    if (parts_of_table(max_blocks, half) > kMaxFine) break;
-    pb = half;
-  }
-  return pb;
-}
-
-// Units that the partials are sized for at least, so that a call with fewer
-// requests never asks for a larger workspace than one with more: halving (or a
-// step from 48 to 16) starts below kFewUnits, so no fine call has more.
-constexpr int64_t kFineUnits = 3 * kFewUnits;
-constexpr float kNegBig = -1.0e30f;
-
-struct DecodeArgs {
-  const uint16_t* q;
-  const uint16_t* k_new;
-  const uint16_t* v_new;
-  uint16_t* k_cache;
-  uint16_t* v_cache;
-  const int32_t* block_table;
-  const int32_t* ctx_lens;
-  const int32_t* block_version;
-  const int32_t* req_version;
-  uint16_t* out;
-  float* lse;
-  float* part_o;   // [B][Hq][n_parts][D]
-  float* part_ml;  // [B][Hq][n_parts][2]  (max in log2 units, sum)
-  // The version check of the same call (null when not asked for): per
-  // (request, partition), the stale blocks as a bit mask (bit i = block
-  // j0 + i) and the live tokens of the valid ones, written by KV head 0's
-  // waves; the merge launch turns them into the canonical outputs.
-  uint64_t* vc_mask;    // [B][n_parts]
-  int32_t* vc_valid;    // [B][n_parts]
-  int32_t* vc_pairs;    // [cap][2] (b, j), or null when cap == 0
-  int64_t vc_cap;
-  int32_t* vc_n_stale;  // one int32
-  int32_t* vc_valid_tokens;  // [B]
-  int64_t num_blocks;
-  int Hq, Hkv, group, max_blocks, n_parts;
-  int pb;            // blocks per partition (part_blocks of max_blocks)
-  float scale_log2;  // sm_scale * log2(e)
-};
-
-// Logical blocks request b owns: ceil(L/16), at most the table's width.
-__device__ __forceinline__ int owned_blocks(int L, int max_blocks) {
-  return L <= 0 ? 0 : min((L + kBlockSize - 1) / kBlockSize, max_blocks);
-}
-
-// Set bits of m below this lane.
-__device__ __forceinline__ int bits_below(uint64_t m) {
-  return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32),
-                                   __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0u));
-}
-
-// Full partitions of nb blocks (part_blocks is 16, 32, 48 or 64).
-__device__ __forceinline__ int full_parts(int nb, int pb) {
-  const unsigned u = static_cast<unsigned>(nb);
-  return static_cast<int>(pb == 48 ? u / 48u : u >> (pb == 16 ? 4 : pb == 32 ? 5 : 6));
-}
-
-// Requests a wavefront ranks at once: 64 per register, up to this many
-// registers (larger batches use the grid order below without ranking).
-constexpr int kRankChunks = 8;
-
-// The unit of work of dispatch slot k, longest first: every full partition,
-// request by request (they are equally long), then each request's partial
-// partition, longest first (ties: smaller b); an empty context is a partial
-// partition of no block. Returns the request (-1 past the last unit) and, in
-// *part, its partition index (a partial one is numbered n_full, as in the
-// merge). Every lane returns the same.
-//
-// Every wave of every slot runs this before it knows what to load, so its
-// instructions count (with 128 requests and 1000 units, 30 us of issue slots over
-// the chip when the partial partitions were searched length by length and
-// the k-th set bit by clearing k of them): the full partitions are found by
-// prefix sums over the bits of n_full, the partial ones by a radix selection
-// over the 6 bits of their length, all with ballots.
-__device__ int decode_unit(const DecodeArgs& a, int B, int k, int* part) {
-  const int lane = threadIdx.x % kWave;
-  const int nc = (B + kWave - 1) / kWave;
-  int nf[kRankChunks], rem[kRankChunks], pre[kRankChunks];
-  uint64_t cand[kRankChunks];  // requests with a partial partition
-#pragma unroll
-  for (int c = 0; c < kRankChunks; ++c) {
-    if (c >= nc) break;
-    const int b = c * kWave + lane;
-    rem[c] = b < B ? a.ctx_lens[b] : -1;
-  }
-  int n_partial = 0;
-#pragma unroll
-  for (int c = 0; c < kRankChunks; ++c) {
-    if (c >= nc) break;
-    const bool in = c * kWave + lane < B;
-    const int nb = in ? owned_blocks(rem[c], a.max_blocks) : 0;
-    nf[c] = full_parts(nb, a.pb);
-    rem[c] = nb - nf[c] * a.pb;
-    cand[c] = __ballot(in && (nb == 0 || rem[c] > 0));
-    n_partial += __popcll(cand[c]);
-  }
-  // exclusive prefix sums of n_full over the requests, bit by bit
-  int full = 0;
-#pragma unroll
-  for (int c = 0; c < kRankChunks; ++c) {
-    if (c >= nc) break;
-    pre[c] = full;
-    for (int bit = 0; (1 << bit) <= a.n_parts; ++bit) {
-      const uint64_t m = __ballot((nf[c] >> bit) & 1);
-      pre[c] += bits_below(m) << bit;
-      full += __popcll(m) << bit;
-    }
-  }
-  if (k >= full + n_partial) return -1;
-  if (k < full) {
-#pragma unroll
-    for (int c = 0; c < kRankChunks; ++c) {
-      if (c >= nc) break;
-      const uint64_t m = __ballot(k >= pre[c] && k < pre[c] + nf[c]);
-      if (m) {
-        const int l = __builtin_ctzll(m);
-        *part = k - __builtin_amdgcn_readlane(pre[c], l);
-        return c * kWave + l;
-      }
-    }
-  }
-  k -= full;
-  for (int bit = 5; bit >= 0; --bit) {  // (a partial partition has at most 63 blocks)
-    int longer = 0;
-#pragma unroll
-    for (int c = 0; c < kRankChunks; ++c) {
-      if (c >= nc) break;
-      longer += __popcll(cand[c] & __ballot((rem[c] >> bit) & 1));
-    }
-    const bool take = k < longer;
-    if (!take) k -= longer;
-#pragma unroll
-    for (int c = 0; c < kRankChunks; ++c) {
-      if (c >= nc) break;
-      const uint64_t m = __ballot((rem[c] >> bit) & 1);
-      cand[c] &= take ? m : ~m;
-    }
-  }
-#pragma unroll
-  for (int c = 0; c < kRankChunks; ++c) {
-    if (c >= nc) break;
-    const int n = __popcll(cand[c]);
-    if (k < n) {
-      const bool mine = (cand[c] >> lane & 1ull) && bits_below(cand[c]) == k;
-      const int l = __builtin_ctzll(__ballot(mine));
-      *part = __builtin_amdgcn_readlane(nf[c], l);
-      return c * kWave + l;
-    }
-    k -= n;
-  }
-  return -1;
-}
 
 // The 4 V values a lane holds for one block (slots slot0..slot0+3), with
 // slots past s_live set to 0 (their cache contents are undefined and must not
@@ -266,15 +81,8 @@ struct BlockRegs {
   u32x2 v[D / 16];
 };
 
-// Bytes of LDS a workgroup of W > 1 waves merges its waves' results in: per
-// (wave, column) an unnormalised O row (padded by 16 bytes, so that the columns
-// a wave writes together fall in distinct banks), its maximum and its sum.
-template <int D>
-constexpr int merge_lds_bytes(int W, int group) {
-  return W * group * (D + 4 + 2) * static_cast<int>(sizeof(float));
-}
-
-template <int D, int DEPTH, bool RANKED, int W>
+// WEIGHTED: each block's share of the softmax is recorded (DecodeArgs::blk_lse).
+template <int D, int DEPTH, bool RANKED, int W, bool WEIGHTED>
 __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int B) {
   constexpr int KC = D / 32;  // 32-dim chunks of the QK product
   constexpr int VT = D / 16;  // 16-dim tiles of the PV product
@@ -343,6 +151,13 @@ __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int
       const int64_t slot = static_cast<int64_t>(b) * a.n_parts + part;
       a.vc_mask[slot] = stale;
       a.vc_valid[slot] = live;
+    }
+  }
+  if constexpr (WEIGHTED) {  // stale blocks of this partition have no weight
+    if (wave == 0 && lane < a.pb && j0 + lane < jend && !ok) {
+      float* bl = a.blk_lse +
+                  (static_cast<int64_t>(b) * a.max_blocks + j0 + lane) * a.Hq + g * G;
+      for (int h = 0; h < G; ++h) bl[h] = -INFINITY;
     }
   }
 
@@ -443,6 +258,8 @@ __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int
     }
     l_run = l_run * alpha + psum;
     m_run = m_new;
+    if constexpr (WEIGHTED)
+      record_block(a, b, j, g * G + col, psum, m_new, kgrp == 0 && col < G);
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       acc[t] *= alpha;
@@ -534,6 +351,10 @@ __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int
         *reinterpret_cast<u32x2*>(a.out + bh * D + d) =
             u32x2{pack_bf16x2(num[0], num[1]), pack_bf16x2(num[2], num[3])};
         if (d == 0 && a.lse) a.lse[bh] = den > 0.f ? (M + __log2f(den)) * kLn2 : -INFINITY;
+        if (WEIGHTED && d == 0) {
+          a.part_ml[bh * a.n_parts * 2] = M;
+          a.part_ml[bh * a.n_parts * 2 + 1] = den;
+        }
       } else {
         const int64_t pi = bh * a.n_parts + part;
         *reinterpret_cast<f32x4*>(a.part_o + pi * D + d) = num;
@@ -555,6 +376,10 @@ __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int
                   pack_bf16x2(acc[t][2] * inv, acc[t][3] * inv)};
       if (kgrp == 0 && a.lse)
         a.lse[bh] = l_run > 0.f ? (m_run + __log2f(l_run)) * kLn2 : -INFINITY;
+      if (WEIGHTED && kgrp == 0) {
+        a.part_ml[bh * a.n_parts * 2] = m_run;
+        a.part_ml[bh * a.n_parts * 2 + 1] = l_run;
+      }
     } else {
       const int64_t pi = bh * a.n_parts + part;
 #pragma unroll
@@ -568,115 +393,6 @@ __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int
   }
 }
 
-// Merge the partitions of every (request, head) that has more than one.
-// The version check from the partitions' stale masks (one workgroup per
-// request, D threads): the request's offset in the canonical list is the
-// number of stale blocks of the requests before it; its own stale blocks
-// follow in ascending j (partitions in descending index). Deterministic, no
-// atomics.
-__device__ void decode_version_check(const DecodeArgs& a, int b, int B, int* sh) {
-  const int tid = threadIdx.x, nt = blockDim.x;
-  auto parts_of = [&](int bb) {
-    const int nbb = owned_blocks(a.ctx_lens[bb], a.max_blocks);
-    return max(1, full_parts(nbb + a.pb - 1, a.pb));
-  };
-  int before = 0;
-  for (int e = tid; e < b * a.n_parts; e += nt) {
-    const int bb = e / a.n_parts, pp = e % a.n_parts;
-    if (pp < parts_of(bb)) before += __popcll(a.vc_mask[e]);
-  }
-  const int np = parts_of(b);
-  // this request's partitions in ascending j: t-th is partition np - 1 - t
-  int cnt = 0, valid = 0;
-  uint64_t mask = 0ull;
-  if (tid < np) {
-    const int64_t slot = static_cast<int64_t>(b) * a.n_parts + (np - 1 - tid);
-    mask = a.vc_mask[slot];
-    cnt = __popcll(mask);
-    valid = a.vc_valid[slot];
-  }
-  // block-wide sums of `before` and `valid`, exclusive prefix of `cnt` over t
-  sh[tid] = cnt;
-  __syncthreads();
-  int pre = 0;
-  for (int t = 0; t < tid && t < np; ++t) pre += sh[t];
-  __syncthreads();
-  sh[tid] = before;
-  __syncthreads();
-  for (int w = nt / 2; w > 0; w >>= 1) {
-    if (tid < w) sh[tid] += sh[tid + w];
-    __syncthreads();
-  }
-  const int offset = sh[0];
-  __syncthreads();
-  sh[tid] = valid;
-  __syncthreads();
-  for (int w = nt / 2; w > 0; w >>= 1) {
-    if (tid < w) sh[tid] += sh[tid + w];
-    __syncthreads();
-  }
-  if (tid == 0) a.vc_valid_tokens[b] = sh[0];
-  if (tid < np) {  // (np <= n_parts <= nt: the host checks)
-    const int nbb = owned_blocks(a.ctx_lens[b], a.max_blocks);
-    const int p = np - 1 - tid;
-    const int j0 = max(0, nbb - a.pb * (p + 1));
-    int64_t pos = static_cast<int64_t>(offset) + pre;
-    for (uint64_t m = mask; m; m &= m - 1ull, ++pos) {
-      if (pos < a.vc_cap) {
-        a.vc_pairs[2 * pos] = b;
-        a.vc_pairs[2 * pos + 1] = j0 + __ffsll(static_cast<long long>(m)) - 1;
-      }
-    }
-    if (b == B - 1 && tid == np - 1) *a.vc_n_stale = offset + pre + cnt;
-  }
-}
-
-template <int D>
-__global__ __launch_bounds__(D) void decode_merge_kernel(DecodeArgs a, int B) {
-  const int bh = blockIdx.x;
-  const int b = bh / a.Hq;
-  const int d = threadIdx.x;
-  if (a.vc_mask && bh % a.Hq == 0) {
-    __shared__ int sh[D];
-    decode_version_check(a, b, B, sh);
-  }
-  const int L = a.ctx_lens[b];
-  const int nb = owned_blocks(L, a.max_blocks);
-  const int np = max(1, full_parts(nb + a.pb - 1, a.pb));
-  if (np == 1) return;  // written by the main kernel
-  // one pass over the partitions, 8 at a time with all their loads in flight;
-  // the running sums are rescaled when a batch raises the maximum
-  constexpr int kMergeBatch = 8;
-  const float* ml = a.part_ml + static_cast<int64_t>(bh) * a.n_parts * 2;
-  const float* po = a.part_o + static_cast<int64_t>(bh) * a.n_parts * D;
-  float M = kNegBig, den = 0.f, num = 0.f;
-  for (int p0 = 0; p0 < np; p0 += kMergeBatch) {
-    float2 mlv[kMergeBatch];
-    float ov[kMergeBatch];
-#pragma unroll
-    for (int q = 0; q < kMergeBatch; ++q) {
-      const bool in = p0 + q < np;
-      mlv[q] = in ? *reinterpret_cast<const float2*>(ml + 2 * (p0 + q)) : float2{kNegBig, 0.f};
-      ov[q] = in ? po[static_cast<int64_t>(p0 + q) * D + d] : 0.f;
-    }
-    float Mb = M;
-#pragma unroll
-    for (int q = 0; q < kMergeBatch; ++q) Mb = fmaxf(Mb, mlv[q].x);
-    const float c = fast_exp2(M - Mb);
-    den *= c;
-    num *= c;
-#pragma unroll
-    for (int q = 0; q < kMergeBatch; ++q) {
-      const float f = fast_exp2(mlv[q].x - Mb);
-      den += mlv[q].y * f;
-      num += ov[q] * f;
-    }
-    M = Mb;
-  }
-  a.out[static_cast<int64_t>(bh) * D + d] = f32_to_bf16(den > 0.f ? num / den : 0.f);
-  if (d == 0 && a.lse) a.lse[bh] = den > 0.f ? (M + __log2f(den)) * kLn2 : -INFINITY;
-}
-
 // Blocks in flight per wave: 4 with one query head per KV head, 3 with
 // grouped heads (measured: 4 is 1.7% faster on the MHA decode step and 1.2%
 // slower on the GQA one, whose waves do four heads' softmax per block).
@@ -687,23 +403,30 @@ __global__ __launch_bounds__(D) void decode_merge_kernel(DecodeArgs a, int B) {
 #define LOCAL_DECODE_DEPTH 3
 #endif
 
-template <int D, int DEPTH, bool RANKED>
+template <int D, int DEPTH, bool RANKED, bool WEIGHTED>
 void launch_attn(const DecodeArgs& a, int B, unsigned grid, int W, hipStream_t s) {
   const int lds = merge_lds_bytes<D>(W, a.group);
   if (W == 4)
-    decode_attn_kernel<D, DEPTH, RANKED, 4><<<grid, 4 * kWave, lds, s>>>(a, B);
+    decode_attn_kernel<D, DEPTH, RANKED, 4, WEIGHTED><<<grid, 4 * kWave, lds, s>>>(a, B);
   else if (W == 2)
-    decode_attn_kernel<D, DEPTH, RANKED, 2><<<grid, 2 * kWave, lds, s>>>(a, B);
+    decode_attn_kernel<D, DEPTH, RANKED, 2, WEIGHTED><<<grid, 2 * kWave, lds, s>>>(a, B);
   else
-    decode_attn_kernel<D, DEPTH, RANKED, 1><<<grid, kWave, 0, s>>>(a, B);
+    decode_attn_kernel<D, DEPTH, RANKED, 1, WEIGHTED><<<grid, kWave, 0, s>>>(a, B);
 }
 
 template <int D, int DEPTH>
 void launch_ranked(const DecodeArgs& a, int B, unsigned grid, int W, hipStream_t s) {
-  if (B <= kRankChunks * kWave)
-    launch_attn<D, DEPTH, true>(a, B, grid, W, s);
-  else
-    launch_attn<D, DEPTH, false>(a, B, grid, W, s);
+  if (B <= kRankChunks * kWave) {
+    if (a.w_out)
+      launch_attn<D, DEPTH, true, true>(a, B, grid, W, s);
+    else
+      launch_attn<D, DEPTH, true, false>(a, B, grid, W, s);
+  } else {
+    if (a.w_out)
+      launch_attn<D, DEPTH, false, true>(a, B, grid, W, s);
+    else
+      launch_attn<D, DEPTH, false, false>(a, B, grid, W, s);
+  }
 }
 
 // Waves that share a partition. What a wave does before its first block (three
@@ -730,17 +453,22 @@ int waves_of(const DecodeArgs& a, int B) {
 
 template <int D>
 local_status_t launch_decode(const DecodeArgs& a, int B, hipStream_t s) {
-  const int64_t wgs = static_cast<int64_t>(a.Hkv) * B * (a.n_parts + 1);
+  const int64_t wgs = std::max(static_cast<int64_t>(a.Hkv) * B * (a.n_parts + 1),
+                               a.w_out ? merge_grid<D>(a, B) : 0);
   if (wgs >= (1LL << 31))
     return local_fail(LOCAL_ERR_UNSUPPORTED, "paged_attn_decode: grid of %lld workgroups",
                       (long long)wgs);
-  const unsigned grid = static_cast<unsigned>(wgs);
+  const unsigned grid = static_cast<unsigned>(a.Hkv) * B * (a.n_parts + 1);
   const int W = waves_of(a, B);
   if (a.group == 1)
     launch_ranked<D, LOCAL_DECODE_DEPTH_MHA>(a, B, grid, W, s);
   else
     launch_ranked<D, LOCAL_DECODE_DEPTH>(a, B, grid, W, s);
-  if (a.n_parts > 1 || a.vc_mask) decode_merge_kernel<D><<<B * a.Hq, D, 0, s>>>(a, B);
+  if (a.w_out)
+    decode_merge_kernel<D, false, true>
+        <<<static_cast<unsigned>(merge_grid<D>(a, B)), D, a.Hq * sizeof(float), s>>>(a, B);
+  else if (a.n_parts > 1 || a.vc_mask)
+    decode_merge_kernel<D, false, false><<<B * a.Hq, D, 0, s>>>(a, B);
   return local_check_launch("paged_attn_decode");
 }
 
@@ -748,31 +476,6 @@ local_status_t launch_decode(const DecodeArgs& a, int B, hipStream_t s) {
 }  // namespace localk
 
 using namespace localk;
-
-// Split-KV partials of a call: the partition length (a->pb, a->n_parts) and what
-// the partials take.
-struct DecodeParts {
-  size_t elems, bytes;  // (request, query head, partition) triples; their bytes
-  size_t units;         // (request, partition) pairs of the version masks
-};
-
-// fine: the partitions that the call's size asks for, with room for any call of
-// fewer requests; else the longest ones of its table and exactly their partials,
-// for a workspace that has no room for more.
-static DecodeParts decode_parts(DecodeArgs& a, int B, int D, bool fine) {
-  a.pb = fine ? part_blocks(a.max_blocks, static_cast<int64_t>(B) * a.Hkv)
-              : longest_part_blocks(a.max_blocks);
-  a.n_parts = parts_of_table(a.max_blocks, a.pb);
-  DecodeParts p;
-  p.units = static_cast<size_t>(B > 0 ? B : 1) * a.n_parts;
-  p.elems = p.units * a.Hq;
-  if (fine) {
-    p.units = std::max(p.units, static_cast<size_t>(kFineUnits));
-    p.elems = std::max(p.elems, static_cast<size_t>(kFineUnits) * a.group);
-  }
-  p.bytes = p.elems * (D + 2) * sizeof(float);
-  return p;
-}
 
 // Host-side validation shared by the entry points: fills *a (without the
 // partials' pointers) and *part, the split-KV partials of the call.
@@ -812,6 +515,11 @@ static local_status_t decode_setup(const uint16_t* q, int32_t B, int32_t Hq, int
   a->vc_cap = 0;
   a->vc_n_stale = nullptr;
   a->vc_valid_tokens = nullptr;
+  a->blk_lse = nullptr;
+  a->w_in = nullptr;
+  a->w_out = nullptr;
+  a->w_decay = 1.f;
+  a->kv4 = nullptr;
   a->Hq = Hq;
   a->Hkv = Hkv;
   a->group = Hq / Hkv;
@@ -879,7 +587,6 @@ extern "C" int32_t localk_decode_form(int32_t B, int32_t Hq, int32_t Hkv, int32_
 // ---------------------------------------------------------------- checked
 namespace {
 __global__ void decode_vc_empty_kernel(int32_t* n_stale) { *n_stale = 0; }
-size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 }  // namespace
 
 extern "C" local_status_t local_paged_attn_decode_checked(
@@ -998,4 +705,45 @@ extern "C" local_status_t local_paged_attn_decode_noalloc(
   void* partials = scratch_of_current_device(&st);
   if (!partials) return st;
   return decode_launch(a, B, D, partials, part.elems, stream);
+}
+
+// ---------------------------------------------------------------- weighted
+// Decode attention with the weight of each block. The attention launch records
+// each (block, query head)'s log-sum-exp as it passes (B * max_blocks * Hq floats:
+// 4 bytes where the block's K and V of one KV head take 64 D), and the merge
+// launch, which knows every head's sum, turns them into weights: no launch and no
+// pass over K of its own.
+extern "C" local_status_t local_paged_attn_decode_weighted(
+    const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+    const uint16_t* k_new, const uint16_t* v_new, uint16_t* k_cache, uint16_t* v_cache,
+    int64_t num_blocks, int32_t block_size, const int32_t* block_table,
+    int32_t max_blocks, const int32_t* ctx_lens, const int32_t* block_version,
+    const int32_t* req_version, float sm_scale, uint16_t* out, float* lse,
+    const float* weight_in, float weight_decay, float* weight_out, void* ws,
+    size_t* ws_bytes, void* stream) {
+  const char* who = "paged_attn_decode_weighted";
+  if (!ws_bytes) return local_fail(LOCAL_ERR_WORKSPACE, "%s: ws_bytes is NULL", who);
+  DecodeArgs a;
+  DecodeParts part;
+  local_status_t st = decode_setup(q, B, Hq, Hkv, D, k_new, v_new, k_cache, v_cache,
+                                   num_blocks, block_size, block_table, max_blocks, ctx_lens,
+                                   block_version, req_version, sm_scale, out, lse, who, &a,
+                                   &part);
+  if (st != LOCAL_OK) return st;
+  if ((st = decode_weights_ok(Hq, weight_decay, who)) != LOCAL_OK) return st;
+  const size_t need = align256(part.bytes) + block_lse_bytes(B, Hq, max_blocks);
+  if (!ws) {
+    *ws_bytes = need;
+    return LOCAL_OK;
+  }
+  if (*ws_bytes < need)
+    return local_fail(LOCAL_ERR_WORKSPACE, "%s: workspace %zu < %zu", who, *ws_bytes, need);
+  if (B == 0) return LOCAL_OK;
+  if ((st = decode_pointers_ok(a, who)) != LOCAL_OK) return st;
+  if (!weight_out) return local_fail(LOCAL_ERR_NULL, "%s: weight_out is NULL", who);
+  a.blk_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(part.bytes));
+  a.w_in = weight_in;
+  a.w_out = weight_out;
+  a.w_decay = weight_decay;
+  return decode_launch(a, B, D, ws, part.elems, stream);
 }

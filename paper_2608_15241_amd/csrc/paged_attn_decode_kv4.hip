@@ -1,0 +1,498 @@
+// local_paged_attn_decode_kv4: decode attention over the 4-bit pool, with the new
+// token's append and, when asked for, the weight of each block.
+//
+// Mathematics: s = sm_scale q K^, w = softmax(s), out = w V^ over the valid keys, K^
+// and V^ the values that the pool's codes stand for (the new token's too). Those are
+// bf16 values exactly, so the products and sums are those of bf16 decode attention.
+//
+// Bound by HBM: a block and KV head is one tile of 17 D bytes, read once, against
+// 64 D in bf16. What the smaller tile changes against the bf16 kernel:
+//  * Unpacking must not cost more than the loads: 2176 bytes hold 4096 values, so at
+//    6 TB/s the chip has some 3 vector instructions a value. The codes lie in operand
+//    order (kv4.hpp), a conversion makes two scaled values, and V needs one lane-local
+//    permute per two values to pair neighbouring tokens: 1.3 instructions a value and
+//    lane group, of which the scales are 0.2.
+//  * Blocks are taken in pairs: the value product then is a 16x16x32 (32 keys), and
+//    the running maximum, the rescale and the cross-lane steps come once a pair.
+//  * Partitions, dispatch order, waves per partition and merge: as for bf16.
+#include "kv4.hpp"
+#include "paged_attn_decode.hpp"
+
+namespace localk {
+namespace {
+
+// One pair of blocks in registers, as loaded.
+template <int D>
+struct Regs4 {
+  uint32_t k[2][D / 32];  // this lane's codes of K and V
+  uint32_t v[2][D / 32];
+  uint32_t ks[2], vs[2];  // the scale of its K dims; the scales of its 4 tokens of V
+};
+
+template <int D>
+__device__ __forceinline__ void load_codes(__amdgpu_buffer_rsrc_t r, uint32_t off,
+                                           uint32_t (&c)[D / 32]) {
+  if constexpr (D == 128) {
+    const u32x4 v = buf_load16_stream(r, off);
+    c[0] = v.x, c[1] = v.y, c[2] = v.z, c[3] = v.w;
+  } else {
+    const u32x2 v = buf_load8_stream(r, off);
+    c[0] = v.x, c[1] = v.y;
+  }
+}
+
+// The new token as a lane holds it: its K dims (D/4, one scale) where the lane's
+// column is the token's slot, its V dims (D/16) where its k-group holds the slot.
+template <int D>
+struct NewToken {
+  uint32_t k[D / 32], v, ks, vs;
+};
+
+template <int D>
+__device__ __forceinline__ void quantise_new(const uint16_t* k_new, const uint16_t* v_new,
+                                             int col, int kgrp, NewToken<D>& n) {
+  float x[D / 32][8];
+  float amax = 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    split8(ld_global<u32x4>(k_new + (D / 4) * kgrp + 8 * c), x[c]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = amax_bits(amax, x[c][i]);
+  }
+  if constexpr (D == 64) amax = amax_xor(amax, 16);  // the group's other 16 dims
+  n.ks = scale_byte(amax);
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) n.k[c] = pack4x8(x[c], n.ks);
+
+  float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if constexpr (D == 128) {
+    split8(ld_global<u32x4>(v_new + 8 * col), y);
+  } else {
+    const u32x2 w = ld_global<u32x2>(v_new + 4 * col);
+    y[0] = lo_bf16(w.x), y[1] = hi_bf16(w.x), y[2] = lo_bf16(w.y), y[3] = hi_bf16(w.y);
+  }
+  amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) amax = amax_bits(amax, y[i]);
+  amax = amax_xor(amax, 1);
+  amax = amax_xor(amax, 2);
+  if constexpr (D == 64) amax = amax_xor(amax, 4);
+  n.vs = scale_byte(amax);
+  n.v = pack4x8(y, n.vs);  // (D = 64: the low half)
+}
+
+template <int D, int DEPTH, bool RANKED, int W, bool WEIGHTED>
+__global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int B) {
+  using L4 = Kv4<D>;
+  constexpr int KC = D / 32;
+  constexpr int VT = D / 16;
+
+  const int lane = threadIdx.x % kWave;
+  const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int col = lane % 16, kgrp = lane / 16;
+  // Units and their order: as decode_attn_kernel.
+  const int g = blockIdx.x % a.Hkv;
+  const int slot = blockIdx.x / a.Hkv;
+  int b, part;
+  if (RANKED) {
+    b = decode_unit(a, B, slot, &part);
+    if (b < 0) return;
+  } else {
+    b = slot % B;
+    part = slot / B;
+  }
+  const int L = a.ctx_lens[b];
+  const int nb = owned_blocks(L, a.max_blocks);
+  const int n_full = full_parts(nb, a.pb), rem = nb - n_full * a.pb;
+  if (!RANKED) {
+    if (part < a.n_parts) {
+      if (part >= n_full && !(nb == 0 && part == 0)) return;
+    } else {
+      if (rem == 0) return;
+      part = n_full;
+    }
+  }
+  const int jend = nb - part * a.pb;
+  const int j0 = max(0, jend - a.pb);
+  const int n_parts_b = max(1, n_full + (rem > 0 ? 1 : 0));
+  const int rv = a.req_version[b];
+  const int32_t* table = a.block_table + static_cast<int64_t>(b) * a.max_blocks;
+  const int G = a.group;
+
+  const bool owned = lane < a.pb && j0 + lane < jend;
+  int my_phys = 0;
+  bool ok = false;
+  if (owned) {
+    my_phys = table[j0 + lane];
+    ok = my_phys >= 0 && my_phys < a.num_blocks && a.block_version[my_phys] == rv;
+    if (!ok) my_phys = 0;  // an id outside the pool is never dereferenced
+  }
+  const uint64_t part_valid = __ballot(ok);
+  uint64_t valid_mask = part_valid;
+  if (W > 1)
+    valid_mask = __ballot(ok && __popcll(part_valid & ((1ull << lane) - 1ull)) % W == wave);
+  if constexpr (WEIGHTED) {  // stale blocks of this partition have no weight
+    if (wave == 0 && owned && !ok) {
+      float* bl = a.blk_lse +
+                  (static_cast<int64_t>(b) * a.max_blocks + j0 + lane) * a.Hq + g * G;
+      for (int h = 0; h < G; ++h) bl[h] = -INFINITY;
+    }
+  }
+
+  // Query heads of this KV head as the B operand (column = head); a lane's dims are
+  // those of its codes of K.
+  bf16x8 qv[KC];
+  {
+    const int h = g * G + col;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (col < G)
+        v = ld_global<u32x4>(a.q + (static_cast<int64_t>(b) * a.Hq + h) * D + (D / 4) * kgrp +
+                             8 * c);
+      qv[c] = as_bf16x8(v);
+    }
+  }
+
+  // The new token (position L-1), if its block is in this partition: substituted while
+  // the block is read, written after the last block.
+  const int j_new = (L - 1) / kBlockSize, s_last = (L - 1) % kBlockSize;
+  const bool has_new = a.k_new != nullptr;
+  bool append = has_new && j_new >= j0 && j_new < jend;
+  if (W > 1 && append)  // by the wave that reads the block (a stale one: wave 0)
+    append = (part_valid >> (j_new - j0) & 1ull) ? (valid_mask >> (j_new - j0) & 1ull) != 0ull
+                                                 : wave == 0;
+  const int p_new = append ? table[j_new] : -1;
+  NewToken<D> fresh{};
+  if (append) {
+    const int64_t row = (static_cast<int64_t>(b) * a.Hkv + g) * D;
+    quantise_new<D>(a.k_new + row, a.v_new + row, col, kgrp, fresh);
+  }
+
+  f32x4 acc[VT];
+#pragma unroll
+  for (int t = 0; t < VT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = kNegBig, l_run = 0.f;
+
+  auto next_block = [&]() -> int {
+    if (!valid_mask) return -1;
+    const int i = __builtin_ctzll(valid_mask);
+    valid_mask &= valid_mask - 1;
+    return i;
+  };
+  auto load_block = [&](Regs4<D>& R, int e, int i) {
+    const bool live = i >= 0;
+    const int p = live ? __builtin_amdgcn_readlane(my_phys, i) : 0;
+    const int64_t tile = (static_cast<int64_t>(p) * a.Hkv + g) * L4::kTile;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.kv4 + tile, live ? L4::kTile : 0u);
+    load_codes<D>(r, lane * L4::kLane, R.k[e]);
+    load_codes<D>(r, L4::kV + lane * L4::kLane, R.v[e]);
+    R.ks[e] = __builtin_amdgcn_raw_buffer_load_b8(r, L4::k_scale(L4::k_group(kgrp), col), 0,
+                                                  kCacheStream);
+    R.vs[e] = __builtin_amdgcn_raw_buffer_load_b32(r, L4::v_scale(L4::v_group(col), 4 * kgrp), 0,
+                                                   kCacheStream);
+  };
+  // The block that holds the last position: the new token's codes for its slot; slots
+  // past it as zeros (their contents are undefined and must not reach the product).
+  auto fix_last = [&](Regs4<D>& R, int e) {
+    if (has_new && col == s_last) {
+#pragma unroll
+      for (int c = 0; c < KC; ++c) R.k[e][c] = fresh.k[c];
+      R.ks[e] = fresh.ks;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = 4 * kgrp + i;
+      const bool dead = s > s_last, put = has_new && s == s_last;
+      const uint32_t byte = 0xffu << (8 * i);
+      R.vs[e] = dead ? R.vs[e] & ~byte : put ? (R.vs[e] & ~byte) | fresh.vs << (8 * i) : R.vs[e];
+      if constexpr (D == 128) {
+        R.v[e][i] = dead ? 0u : put ? fresh.v : R.v[e][i];
+      } else {
+        const int sh = 16 * (i % 2);
+        const uint32_t rest = R.v[e][i / 2] & ~(0xffffu << sh);
+        R.v[e][i / 2] = dead ? rest : put ? rest | (fresh.v & 0xffffu) << sh : R.v[e][i / 2];
+      }
+    }
+  };
+  auto compute = [&](Regs4<D>& R, int i0, int i1) {
+    f32x4 sc[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = e ? i1 : i0;
+      if (j0 + i == j_new && i >= 0) fix_last(R, e);
+      const float ks = scale4(R.ks[e]);
+      sc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const uint32_t w = R.k[e][c];
+        const u32x4 kf = {unpack4<0>(w, ks), unpack4<1>(w, ks), unpack4<2>(w, ks),
+                          unpack4<3>(w, ks)};
+        sc[e] = mfma16x16x32(as_bf16x8(kf), qv[c], sc[e]);
+      }
+    }
+    float s[2][4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = e ? i1 : i0;
+      const int live = i < 0 ? 0 : L - (j0 + i) * kBlockSize;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        s[e][k] = 4 * kgrp + k < live ? sc[e][k] * a.scale_log2 : -INFINITY;
+    }
+    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    mx = max_xor32(max_xor16(mx));
+    const float m_new = fmaxf(m_run, mx);
+    const float alpha = fast_exp2(m_run - m_new);
+    float ps[2] = {0.f, 0.f};
+    u32x4 pf;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float p[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        p[k] = fast_exp2(s[e][k] - m_new);
+        ps[e] += p[k];
+      }
+      pf[2 * e] = pack_bf16x2(p[0], p[1]);
+      pf[2 * e + 1] = pack_bf16x2(p[2], p[3]);
+    }
+    l_run = l_run * alpha + (ps[0] + ps[1]);
+    m_run = m_new;
+    if constexpr (WEIGHTED) {
+      record_block(a, b, j0 + i0, g * G + col, ps[0], m_new, kgrp == 0 && col < G);
+      record_block(a, b, j0 + i1, g * G + col, ps[1], m_new, kgrp == 1 && col < G && i1 >= 0);
+    }
+    u32x2 va[VT], vb[VT];
+    unpack_v<D>(R.v[0], R.vs[0], va);
+    unpack_v<D>(R.v[1], R.vs[1], vb);
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      acc[t] *= alpha;
+      acc[t] = mfma16x16x32(as_bf16x8(u32x4{va[t].x, va[t].y, vb[t].x, vb[t].y}), as_bf16x8(pf),
+                            acc[t]);
+    }
+  };
+
+  // ring of DEPTH pairs: DEPTH-1 pairs load while one computes
+  Regs4<D> R[DEPTH];
+  int i0[DEPTH], i1[DEPTH];
+  auto fill = [&](int d) {
+    i0[d] = next_block();
+    i1[d] = next_block();
+    load_block(R[d], 0, i0[d]);
+    load_block(R[d], 1, i1[d]);
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH - 1; ++d) fill(d);
+  bool done = false;
+  while (!done) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      fill((d + DEPTH - 1) % DEPTH);
+      if (i0[d] < 0) {
+        done = true;
+        break;
+      }
+      compute(R[d], i0[d], i1[d]);
+    }
+  }
+
+  // ---- append, after every read of the block
+  if (append && p_new >= 0 && p_new < a.num_blocks) {
+    uint8_t* tile = a.kv4 + (static_cast<int64_t>(p_new) * a.Hkv + g) * L4::kTile;
+    if (col == 0) {  // K: the slot's codes of each k-group
+      uint32_t* to = reinterpret_cast<uint32_t*>(tile + (kgrp * kBlockSize + s_last) * L4::kLane);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) to[c] = fresh.k[c];
+      if (D == 128 || kgrp % 2 == 0)
+        tile[L4::k_scale(L4::k_group(kgrp), s_last)] = static_cast<uint8_t>(fresh.ks);
+    }
+    if (kgrp == 1) {  // V: the slot's codes of each column's dims
+      uint8_t* to = tile + L4::kV + ((s_last / 4 * 16 + col) * 4 + s_last % 4) * L4::kTokenV;
+      if constexpr (D == 128)
+        *reinterpret_cast<uint32_t*>(to) = fresh.v;
+      else
+        *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(fresh.v);
+      if (col % (16 / L4::kGroups) == 0)
+        tile[L4::v_scale(L4::v_group(col), s_last)] = static_cast<uint8_t>(fresh.vs);
+    }
+  }
+
+  // ---- finish: the column's sum over the k-groups, then write. Accumulator t, row
+  // 4 kgrp + i is dim (4 kgrp + i) * VT + t, so a lane's dims are 4 * VT neighbours.
+  l_run = sum_kgroups(l_run);
+  const int64_t bh0 = static_cast<int64_t>(b) * a.Hq + g * G;
+  auto put = [&](int hc, int d, f32x4 num, float M, float den) {
+    const int64_t bh = bh0 + hc;
+    if (n_parts_b == 1) {
+      num *= den == 0.f ? 0.f : 1.f / den;
+      *reinterpret_cast<u32x2*>(a.out + bh * D + d) =
+          u32x2{pack_bf16x2(num[0], num[1]), pack_bf16x2(num[2], num[3])};
+      if (d == 0 && a.lse) a.lse[bh] = den == 0.f ? -INFINITY : (M + __log2f(den)) * kLn2;
+    } else {
+      *reinterpret_cast<f32x4*>(a.part_o + (bh * a.n_parts + part) * D + d) = num;
+    }
+    if (d == 0 && (WEIGHTED || n_parts_b > 1)) {
+      const int64_t at = (bh * a.n_parts + part) * 2;
+      a.part_ml[at] = M;
+      a.part_ml[at + 1] = den;
+    }
+  };
+  auto lane_dims = [&](int i, int t4) {  // accumulators 4 t4 .. + 3 of row 4 kgrp + i
+    return f32x4{acc[4 * t4][i], acc[4 * t4 + 1][i], acc[4 * t4 + 2][i], acc[4 * t4 + 3][i]};
+  };
+  if constexpr (W > 1) {
+    extern __shared__ __attribute__((aligned(16))) float mg[];
+    constexpr int kRow = D + 4;
+    float* mg_ml = mg + W * G * kRow;
+    if (col < G) {
+      const int row = wave * G + col;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t4 = 0; t4 < VT / 4; ++t4)
+          *reinterpret_cast<f32x4*>(mg + row * kRow + (4 * kgrp + i) * VT + 4 * t4) =
+              lane_dims(i, t4);
+      if (kgrp == 0) {
+        mg_ml[2 * row] = m_run;
+        mg_ml[2 * row + 1] = l_run;
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < G * (D / 4); e += kWave * W) {
+      const int hc = e / (D / 4), d = 4 * (e % (D / 4));
+      float M = kNegBig;
+#pragma unroll
+      for (int w = 0; w < W; ++w) M = fmaxf(M, mg_ml[2 * (w * G + hc)]);
+      float den = 0.f;
+      f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < W; ++w) {  // a wave without a block: weight x 0
+        const int row = w * G + hc;
+        const float f = fast_exp2(mg_ml[2 * row] - M);
+        den += mg_ml[2 * row + 1] * f;
+        num += *reinterpret_cast<const f32x4*>(mg + row * kRow + d) * f;
+      }
+      put(hc, d, num, M, den);
+    }
+  } else if (col < G) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t4 = 0; t4 < VT / 4; ++t4)
+        put(col, (4 * kgrp + i) * VT + 4 * t4, lane_dims(i, t4), m_run, l_run);
+  }
+}
+
+constexpr int kKv4Depth = 2;  // pairs of blocks in registers
+
+template <int D, bool RANKED, bool WEIGHTED>
+void launch_kv4(const DecodeArgs& a, int B, unsigned grid, int W, hipStream_t s) {
+  const int lds = merge_lds_bytes<D>(W, a.group);
+  if (W == 4)
+    decode_kv4_kernel<D, kKv4Depth, RANKED, 4, WEIGHTED><<<grid, 4 * kWave, lds, s>>>(a, B);
+  else if (W == 2)
+    decode_kv4_kernel<D, kKv4Depth, RANKED, 2, WEIGHTED><<<grid, 2 * kWave, lds, s>>>(a, B);
+  else
+    decode_kv4_kernel<D, kKv4Depth, RANKED, 1, WEIGHTED><<<grid, kWave, 0, s>>>(a, B);
+}
+
+int kv4_waves(const DecodeArgs& a, int B) {
+  const int64_t units = static_cast<int64_t>(a.Hkv) * B * a.n_parts;
+  return units < 512 ? 4 : units < 2048 ? 2 : 1;
+}
+
+template <int D>
+local_status_t launch_decode_kv4(const DecodeArgs& a, int B, hipStream_t s) {
+  const int64_t wgs = static_cast<int64_t>(a.Hkv) * B * (a.n_parts + 1);
+  const int64_t merge = merge_grid<D>(a, B);
+  if (std::max(wgs, merge) >= (1LL << 31))
+    return local_fail(LOCAL_ERR_UNSUPPORTED, "paged_attn_decode_kv4: grid of %lld workgroups",
+                      (long long)std::max(wgs, merge));
+  const unsigned grid = static_cast<unsigned>(wgs);
+  const int W = kv4_waves(a, B);
+  if (B <= kRankChunks * kWave)
+    a.w_out ? launch_kv4<D, true, true>(a, B, grid, W, s)
+            : launch_kv4<D, true, false>(a, B, grid, W, s);
+  else
+    a.w_out ? launch_kv4<D, false, true>(a, B, grid, W, s)
+            : launch_kv4<D, false, false>(a, B, grid, W, s);
+  if (a.w_out)
+    decode_merge_kernel<D, true, true>
+        <<<static_cast<unsigned>(merge), D, a.Hq * sizeof(float), s>>>(a, B);
+  else if (a.n_parts > 1)
+    decode_merge_kernel<D, true, false><<<static_cast<unsigned>(merge), D, 0, s>>>(a, B);
+  return local_check_launch("paged_attn_decode_kv4");
+}
+
+}  // namespace
+}  // namespace localk
+
+using namespace localk;
+
+extern "C" local_status_t local_paged_attn_decode_kv4(
+    const uint16_t* q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+    const uint16_t* k_new, const uint16_t* v_new, uint8_t* kv4, int64_t num_blocks,
+    int32_t block_size, const int32_t* block_table, int32_t max_blocks,
+    const int32_t* ctx_lens, const int32_t* block_version, const int32_t* req_version,
+    float sm_scale, uint16_t* out, float* lse, const float* weight_in, float weight_decay,
+    float* weight_out, void* ws, size_t* ws_bytes, void* stream) {
+  const char* who = "paged_attn_decode_kv4";
+  if (!ws_bytes) return local_fail(LOCAL_ERR_WORKSPACE, "%s: ws_bytes is NULL", who);
+  if (B < 0 || Hq <= 0 || Hkv <= 0 || max_blocks < 1 || num_blocks < 1 || Hq % Hkv != 0)
+    return local_fail(LOCAL_ERR_SHAPE, "%s: B=%d Hq=%d Hkv=%d max_blocks=%d num_blocks=%lld",
+                      who, B, Hq, Hkv, max_blocks, (long long)num_blocks);
+  if (block_size != kBlockSize || (D != 64 && D != 128) || Hq / Hkv > 16)
+    return local_fail(LOCAL_ERR_UNSUPPORTED,
+                      "%s: block_size=%d D=%d group=%d (need 16, 64|128, <=16)", who,
+                      block_size, D, Hq / Hkv);
+  if ((k_new == nullptr) != (v_new == nullptr))
+    return local_fail(LOCAL_ERR_NULL, "%s: k_new and v_new must both be set", who);
+  if (weight_in && !weight_out)
+    return local_fail(LOCAL_ERR_NULL, "%s: weight_in without weight_out", who);
+  local_status_t st = decode_weights_ok(Hq, weight_decay, who);
+  if (st != LOCAL_OK) return st;
+  DecodeArgs a{};
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.kv4 = kv4;
+  a.block_table = block_table;
+  a.ctx_lens = ctx_lens;
+  a.block_version = block_version;
+  a.req_version = req_version;
+  a.out = out;
+  a.lse = lse;
+  a.num_blocks = num_blocks;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.group = Hq / Hkv;
+  a.max_blocks = max_blocks;
+  a.scale_log2 = sm_scale * kLog2e;
+  const DecodeParts part = decode_parts(a, B, D, true);
+  // (the same with and without weights, so that one query serves both)
+  const size_t need = align256(part.bytes) + block_lse_bytes(B, Hq, max_blocks);
+  if (!ws) {
+    *ws_bytes = need;
+    return LOCAL_OK;
+  }
+  if (*ws_bytes < need)
+    return local_fail(LOCAL_ERR_WORKSPACE, "%s: workspace %zu < %zu", who, *ws_bytes, need);
+  if (B == 0) return LOCAL_OK;
+  if (!q || !kv4 || !block_table || !ctx_lens || !block_version || !req_version || !out)
+    return local_fail(LOCAL_ERR_NULL, "%s: NULL pointer argument", who);
+  if (!aligned16(q) || !aligned16(kv4) || !aligned16(out) || !aligned16(k_new) ||
+      !aligned16(v_new) || !aligned16(ws))
+    return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: q, k_new, v_new, kv4, out and ws must start "
+                      "on 16 bytes", who);
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = a.part_o + part.elems * D;
+  a.blk_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(part.bytes));
+  a.w_in = weight_in;
+  a.w_out = weight_out;
+  a.w_decay = weight_decay;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return D == 64 ? launch_decode_kv4<64>(a, B, s) : launch_decode_kv4<128>(a, B, s);
+}
