@@ -647,8 +647,7 @@ local_status_t local_paged_attn_decode_kv4(
  *  whose values are not finite does not reach it.
  *  Sizes and errors as local_paged_attn_prefill, T * Hq / Hkv below 2^30; q, k_new,
  *  v_new, kv4, out and ws must start on 16 bytes (LOCAL_ERR_UNSUPPORTED
- *  otherwise). Workspace: the size asked for, which may be 0 (ws must then
- *  still not be NULL, or the call is taken for the query).
+ *  otherwise). Workspace: the size asked for.
  */
 local_status_t local_paged_attn_prefill_kv4(
     const uint16_t* q, const int32_t* q_indptr, int32_t B, int64_t T,

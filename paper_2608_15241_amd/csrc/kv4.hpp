@@ -49,7 +49,7 @@ __device__ __forceinline__ float scale4(uint32_t byte) { return __uint_as_float(
 // Byte i of a dword of scales.
 template <int I>
 __device__ __forceinline__ float scale4_of(uint32_t w) {
-  return __uint_as_float((I < 3 ? w << (23 - 8 * I) : w >> 1) & 0x7f800000u);
+  return __uint_as_float((w >> (8 * I) & 0xffu) << 23);
 }
 
 // Byte SEL of a dword of codes -> two scaled bf16 values (low = low nibble).
@@ -144,6 +144,63 @@ __device__ __forceinline__ void unpack_v(const uint32_t (&v)[D / 32], uint32_t v
 // Maximum of a nonnegative float's bits over lanes l ^ mask.
 __device__ __forceinline__ float amax_xor(float v, int mask) {
   return amax_bits(v, __shfl_xor(v, mask));
+}
+
+// A lane's D/4 dims of one token of K (bf16 pairs; k-group lane / 16) -> codes; returns
+// the scale byte of their group.
+template <int D>
+__device__ __forceinline__ uint32_t round_k(const u32x4 (&kv)[D / 32], uint32_t (&code)[D / 32]) {
+  float x[D / 32][8], amax = 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    split8(kv[c], x[c]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = amax_bits(amax, x[c][i]);
+  }
+  if constexpr (D == 64) amax = amax_xor(amax, 16);  // the group's other 16 dims
+  const uint32_t s = scale_byte(amax);
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) code[c] = pack4x8(x[c], s);
+  return s;
+}
+
+// A lane's D/16 dims of one token of V (bf16 pairs; column lane % 16; D = 64: the first
+// two dwords) -> codes (D = 64: the low half); returns the scale byte of their group.
+template <int D>
+__device__ __forceinline__ uint32_t round_v(u32x4 v, uint32_t& code) {
+  float x[8], amax = 0.f;
+  split8(v, x);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) amax = amax_bits(amax, x[i]);
+  amax = amax_xor(amax, 1);
+  amax = amax_xor(amax, 2);
+  if constexpr (D == 64) amax = amax_xor(amax, 4);
+  const uint32_t s = scale_byte(amax);
+  code = pack4x8(x, s);
+  return s;
+}
+
+constexpr size_t round256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
+
+// max(a, b, c) in one instruction
+__device__ __forceinline__ float max3f(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// Softmax scale in log2 units, kept positive so that the largest raw score is the
+// largest score: a negative scale flips q's signs, a zero one (every visible key then
+// weighs the same) clears q.
+struct Scale4 {
+  float log2;
+  uint32_t q_xor, q_and;
+};
+
+inline Scale4 scale_of(float sm_scale) {
+  const float l = sm_scale * kLog2e;
+  if (l == 0.f) return {1.f, 0u, 0u};
+  return {l < 0.f ? -l : l, l < 0.f ? 0x80008000u : 0u, 0xffffffffu};
 }
 
 // Bytes of the pool that an alignment check asks for: lanes read 16 bytes.

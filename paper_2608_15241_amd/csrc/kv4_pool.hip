@@ -52,38 +52,25 @@ __global__ __launch_bounds__(kPoolWaves* kWave) void kv4_import_kernel(PoolArgs 
   for (int t = 0; t < VT; ++t)
     vv[t] = ld_global<u32x2>(v + (VT * col + t) * kBlockSize + 4 * kgrp);
 
-  float x[D / 32][8], amax = 0.f;
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    split8(kv[c], x[c]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) amax = amax_bits(amax, x[c][i]);
-  }
-  if constexpr (D == 64) amax = amax_xor(amax, 16);
-  const uint32_t ks = scale_byte(amax);
+  uint32_t kc[D / 32];
+  const uint32_t ks = round_k<D>(kv, kc);
   uint32_t* ko = reinterpret_cast<uint32_t*>(o + lane * L4::kLane);
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) ko[c] = pack4x8(x[c], ks);
+  for (int c = 0; c < D / 32; ++c) ko[c] = kc[c];
   if (D == 128 || kgrp % 2 == 0)
     o[L4::k_scale(L4::k_group(kgrp), col)] = static_cast<uint8_t>(ks);
 
   uint32_t vs = 0u, code[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    float m = 0.f;
+  for (int e = 0; e < 4; ++e) {  // token e of the lane's four: its dims as pairs
+    u32x4 y = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      const uint32_t w = e < 2 ? vv[t].x : vv[t].y;
-      y[t] = e % 2 ? hi_bf16(w) : lo_bf16(w);
-      m = amax_bits(m, y[t]);
+    for (int i = 0; i < VT / 2; ++i) {
+      const uint32_t w0 = e < 2 ? vv[2 * i].x : vv[2 * i].y;
+      const uint32_t w1 = e < 2 ? vv[2 * i + 1].x : vv[2 * i + 1].y;
+      y[i] = __builtin_amdgcn_perm(w1, w0, e % 2 ? 0x07060302u : 0x05040100u);
     }
-    m = amax_xor(m, 1);
-    m = amax_xor(m, 2);
-    if constexpr (D == 64) m = amax_xor(m, 4);
-    const uint32_t s = scale_byte(m);
-    vs |= s << (8 * e);
-    code[e] = pack4x8(y, s);
+    vs |= round_v<D>(y, code[e]) << (8 * e);
   }
   uint32_t* vo = reinterpret_cast<uint32_t*>(o + L4::kV + lane * L4::kLane);
   if constexpr (D == 128) {

@@ -155,8 +155,7 @@ __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int
   }
   if constexpr (WEIGHTED) {  // stale blocks of this partition have no weight
     if (wave == 0 && lane < a.pb && j0 + lane < jend && !ok) {
-      float* bl = a.blk_lse +
-                  (static_cast<int64_t>(b) * a.max_blocks + j0 + lane) * a.Hq + g * G;
+      float* bl = blk_lse_at(a, b, g, j0 + lane);
       for (int h = 0; h < G; ++h) bl[h] = -INFINITY;
     }
   }
@@ -258,8 +257,10 @@ __global__ __launch_bounds__(kWave* W) void decode_attn_kernel(DecodeArgs a, int
     }
     l_run = l_run * alpha + psum;
     m_run = m_new;
-    if constexpr (WEIGHTED)
-      record_block(a, b, j, g * G + col, psum, m_new, kgrp == 0 && col < G);
+    if constexpr (WEIGHTED) {  // (log2 of 0 is -inf)
+      const float sum = sum_kgroups(psum);
+      if (kgrp == 0 && col < G) blk_lse_at(a, b, g, j)[col] = m_new + __log2f(sum);
+    }
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       acc[t] *= alpha;
@@ -520,6 +521,8 @@ static local_status_t decode_setup(const uint16_t* q, int32_t B, int32_t Hq, int
   a->w_out = nullptr;
   a->w_decay = 1.f;
   a->kv4 = nullptr;
+  a->q_xor = 0u;
+  a->q_and = ~0u;
   a->Hq = Hq;
   a->Hkv = Hkv;
   a->group = Hq / Hkv;

@@ -83,11 +83,12 @@ struct DecodeArgs {
   // (request, block, query head) the log2 of the sum of exp2(scores) over the
   // block's keys, -inf for a stale block; the merge launch turns it into weights
   // once it knows each head's sum over all blocks.
-  float* blk_lse;  // [B][max_blocks][Hq]
+  float* blk_lse;  // [B][Hkv][max_blocks][group]
   const float* w_in;
   float* w_out;    // [B][max_blocks]
   float w_decay;
   uint8_t* kv4;    // the 4-bit pool, instead of k_cache and v_cache
+  uint32_t q_xor, q_and;  // (4-bit pool) the sign of sm_scale on q's bits, or none of it
 };
 
 constexpr size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
@@ -287,21 +288,47 @@ __device__ void decode_block_weights(const DecodeArgs& a, int unit, float* lse2)
   const int b = unit / chunks, j = unit % chunks * D + static_cast<int>(threadIdx.x);
   const int nb = owned_blocks(a.ctx_lens[b], a.max_blocks);
   const int np = max(1, full_parts(nb + a.pb - 1, a.pb));
-  for (int h = threadIdx.x; h < a.Hq; h += D) {
-    const float2* ml = reinterpret_cast<const float2*>(
-        a.part_ml + (static_cast<int64_t>(b) * a.Hq + h) * a.n_parts * 2);
-    float M = kNegBig, den = 0.f;
-    for (int p = 0; p < np; ++p) M = fmaxf(M, ml[p].x);
-    for (int p = 0; p < np; ++p) den += ml[p].y * fast_exp2(ml[p].x - M);
-    lse2[h] = den == 0.f ? 0.f : M + __log2f(den);  // (no valid key: every blk_lse is -inf)
+  if (unit % chunks * D < nb) {
+    constexpr int kPer = 4;  // lanes that share a head's partitions
+    const int p0 = threadIdx.x % kPer;
+    for (int h0 = 0; h0 < a.Hq; h0 += D / kPer) {
+      const int h = min(h0 + static_cast<int>(threadIdx.x) / kPer, a.Hq - 1);
+      const float2* ml = reinterpret_cast<const float2*>(
+          a.part_ml + (static_cast<int64_t>(b) * a.Hq + h) * a.n_parts * 2);
+      float M = kNegBig, den = 0.f;
+      for (int p = p0; p < np; p += kPer) {
+        const float2 v = ml[p];
+        const float Mn = fmaxf(M, v.x);
+        den = den * fast_exp2(M - Mn) + v.y * fast_exp2(v.x - Mn);
+        M = Mn;
+      }
+      float top = fmaxf(M, __shfl_xor(M, 1));
+      top = fmaxf(top, __shfl_xor(top, 2));
+      den *= fast_exp2(M - top);
+      den += __shfl_xor(den, 1);
+      den += __shfl_xor(den, 2);
+      // (no valid key: every blk_lse is -inf)
+      if (p0 == 0) lse2[h] = den == 0.f ? 0.f : top + __log2f(den);
+    }
   }
   __syncthreads();
   if (j >= a.max_blocks) return;
   const int64_t at = static_cast<int64_t>(b) * a.max_blocks + j;
   float w = 0.f;
   if (j < nb) {
-    const float* bl = a.blk_lse + at * a.Hq;
-    for (int h = 0; h < a.Hq; ++h) w += fast_exp2(bl[h] - lse2[h]);
+    for (int g = 0; g < a.Hkv; ++g) {
+      const float* bl =
+          a.blk_lse + ((static_cast<int64_t>(b) * a.Hkv + g) * a.max_blocks + j) * a.group;
+      const float* l = lse2 + g * a.group;
+      int e = 0;
+      if (a.group % 4 == 0)
+        for (; e < a.group; e += 4) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(bl + e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w += fast_exp2(v[i] - l[e + i]);
+        }
+      for (; e < a.group; ++e) w += fast_exp2(bl[e] - l[e]);
+    }
     if (a.w_in) w = fmaf(a.w_decay, a.w_in[at], w);
   }
   a.w_out[at] = w;
@@ -386,8 +413,7 @@ inline size_t block_lse_bytes(int B, int Hq, int max_blocks) {
   return align256(static_cast<size_t>(B > 0 ? B : 1) * Hq * max_blocks * sizeof(float));
 }
 
-// Records a block's weight: the sum of each column's exp2(score - m) over the 16
-// keys (psum: this lane's 4 keys), by the lanes of k-group `who`.
+// Sum of v over the k-groups (lanes l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float sum_kgroups(float v) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
                                                   false);
@@ -397,12 +423,19 @@ __device__ __forceinline__ float sum_kgroups(float v) {
   return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
-__device__ __forceinline__ void record_block(const DecodeArgs& a, int b, int j, int h, float psum,
-                                             float m, bool mine) {
-  const float sum = sum_kgroups(psum);
-  if (mine)
-    a.blk_lse[(static_cast<int64_t>(b) * a.max_blocks + j) * a.Hq + h] =
-        sum == 0.f ? -INFINITY : m + __log2f(sum);
+// The same of two values at once: k-groups 0 and 2 return the sum of a, 1 and 3 of b.
+__device__ __forceinline__ float sum_kgroups2(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false,
+                                                  false);
+  const float v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+// Where block j of request b, KV head g, records its heads' weights.
+__device__ __forceinline__ float* blk_lse_at(const DecodeArgs& a, int b, int g, int j) {
+  return a.blk_lse + ((static_cast<int64_t>(b) * a.Hkv + g) * a.max_blocks + j) * a.group;
 }
 
 // Split-KV partials of a call: the partition length (a->pb, a->n_parts) and what

@@ -51,38 +51,25 @@ struct NewToken {
 template <int D>
 __device__ __forceinline__ void quantise_new(const uint16_t* k_new, const uint16_t* v_new,
                                              int col, int kgrp, NewToken<D>& n) {
-  float x[D / 32][8];
-  float amax = 0.f;
+  u32x4 kv[D / 32], vv = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    split8(ld_global<u32x4>(k_new + (D / 4) * kgrp + 8 * c), x[c]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) amax = amax_bits(amax, x[c][i]);
-  }
-  if constexpr (D == 64) amax = amax_xor(amax, 16);  // the group's other 16 dims
-  n.ks = scale_byte(amax);
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c) n.k[c] = pack4x8(x[c], n.ks);
-
-  float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < D / 32; ++c) kv[c] = ld_global<u32x4>(k_new + (D / 4) * kgrp + 8 * c);
   if constexpr (D == 128) {
-    split8(ld_global<u32x4>(v_new + 8 * col), y);
+    vv = ld_global<u32x4>(v_new + 8 * col);
   } else {
     const u32x2 w = ld_global<u32x2>(v_new + 4 * col);
-    y[0] = lo_bf16(w.x), y[1] = hi_bf16(w.x), y[2] = lo_bf16(w.y), y[3] = hi_bf16(w.y);
+    vv = u32x4{w.x, w.y, 0u, 0u};
   }
-  amax = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) amax = amax_bits(amax, y[i]);
-  amax = amax_xor(amax, 1);
-  amax = amax_xor(amax, 2);
-  if constexpr (D == 64) amax = amax_xor(amax, 4);
-  n.vs = scale_byte(amax);
-  n.v = pack4x8(y, n.vs);  // (D = 64: the low half)
+  n.ks = round_k<D>(kv, n.k);
+  n.vs = round_v<D>(vv, n.v);
 }
 
+constexpr float kLazy4 = 8.f;  // log2 of the largest weight before the maximum rises
+
+// __launch_bounds__: three waves a SIMD (registers permitting, and they do: two ran the
+// 128 contexts of 1K to 16K tokens 3% slower).
 template <int D, int DEPTH, bool RANKED, int W, bool WEIGHTED>
-__global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int B) {
+__global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, int B) {
   using L4 = Kv4<D>;
   constexpr int KC = D / 32;
   constexpr int VT = D / 16;
@@ -133,9 +120,8 @@ __global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int 
     valid_mask = __ballot(ok && __popcll(part_valid & ((1ull << lane) - 1ull)) % W == wave);
   if constexpr (WEIGHTED) {  // stale blocks of this partition have no weight
     if (wave == 0 && owned && !ok) {
-      float* bl = a.blk_lse +
-                  (static_cast<int64_t>(b) * a.max_blocks + j0 + lane) * a.Hq + g * G;
-      for (int h = 0; h < G; ++h) bl[h] = -INFINITY;
+      float* none = blk_lse_at(a, b, g, j0 + lane);
+      for (int h = 0; h < G; ++h) none[h] = -INFINITY;
     }
   }
 
@@ -150,7 +136,7 @@ __global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int 
       if (col < G)
         v = ld_global<u32x4>(a.q + (static_cast<int64_t>(b) * a.Hq + h) * D + (D / 4) * kgrp +
                              8 * c);
-      qv[c] = as_bf16x8(v);
+      qv[c] = as_bf16x8((v ^ a.q_xor) & a.q_and);
     }
   }
 
@@ -173,6 +159,10 @@ __global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int 
 #pragma unroll
   for (int t = 0; t < VT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = kNegBig, l_run = 0.f;
+  const float inv_scale = 1.f / a.scale_log2;
+  float rise = (kNegBig + kLazy4) * inv_scale;  // a raw score above it raises m_run
+  // (WEIGHTED) where this lane records block j0's weight
+  float* bl = blk_lse_at(a, b, g, j0) + col;
 
   auto next_block = [&]() -> int {
     if (!valid_mask) return -1;
@@ -188,9 +178,9 @@ __global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int 
     load_codes<D>(r, lane * L4::kLane, R.k[e]);
     load_codes<D>(r, L4::kV + lane * L4::kLane, R.v[e]);
     R.ks[e] = __builtin_amdgcn_raw_buffer_load_b8(r, L4::k_scale(L4::k_group(kgrp), col), 0,
-                                                  kCacheStream);
+                                                  0);
     R.vs[e] = __builtin_amdgcn_raw_buffer_load_b32(r, L4::v_scale(L4::v_group(col), 4 * kgrp), 0,
-                                                   kCacheStream);
+                                                   0);
   };
   // The block that holds the last position: the new token's codes for its slot; slots
   // past it as zeros (their contents are undefined and must not reach the product).
@@ -220,7 +210,8 @@ __global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int 
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int i = e ? i1 : i0;
-      if (j0 + i == j_new && i >= 0) fix_last(R, e);
+      const bool tail = i < 0 || j0 + i == j_new;
+      if (tail && i >= 0) fix_last(R, e);
       const float ks = scale4(R.ks[e]);
       sc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -230,49 +221,50 @@ __global__ __launch_bounds__(kWave* W) void decode_kv4_kernel(DecodeArgs a, int 
                           unpack4<3>(w, ks)};
         sc[e] = mfma16x16x32(as_bf16x8(kf), qv[c], sc[e]);
       }
-    }
-    float s[2][4];
+      if (tail) {  // no block, or one with slots past the context's end
+        const int live = i < 0 ? 0 : L - (j0 + i) * kBlockSize;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int i = e ? i1 : i0;
-      const int live = i < 0 ? 0 : L - (j0 + i) * kBlockSize;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        s[e][k] = 4 * kgrp + k < live ? sc[e][k] * a.scale_log2 : -INFINITY;
+        for (int k = 0; k < 4; ++k) sc[e][k] = 4 * kgrp + k < live ? sc[e][k] : -INFINITY;
+      }
     }
-    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    mx = max_xor32(max_xor16(mx));
-    const float m_new = fmaxf(m_run, mx);
-    const float alpha = fast_exp2(m_run - m_new);
-    float ps[2] = {0.f, 0.f};
+    // The running maximum rises only when a weight would pass 2^kLazy4: below, the
+    // weights are exact all the same, and nothing has to cross lanes or be rescaled.
+    const float mx = max3f(max3f(sc[0][0], sc[0][1], sc[0][2]),
+                           max3f(sc[0][3], sc[1][0], sc[1][1]), max2f(sc[1][2], sc[1][3]));
+    if (__ballot(mx > rise)) {
+      const float m_new = fmaxf(m_run, max_xor32(max_xor16(mx)) * a.scale_log2);
+      const float alpha = fast_exp2(m_run - m_new);
+      l_run *= alpha;
+      m_run = m_new;
+      rise = (m_new + kLazy4) * inv_scale;
+#pragma unroll
+      for (int t = 0; t < VT; ++t) acc[t] *= alpha;
+    }
+    float ps[2];
     u32x4 pf;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float p[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        p[k] = fast_exp2(s[e][k] - m_new);
-        ps[e] += p[k];
-      }
+      for (int k = 0; k < 4; ++k) p[k] = fast_exp2(fmaf(sc[e][k], a.scale_log2, -m_run));
+      ps[e] = (p[0] + p[1]) + (p[2] + p[3]);
       pf[2 * e] = pack_bf16x2(p[0], p[1]);
       pf[2 * e + 1] = pack_bf16x2(p[2], p[3]);
     }
-    l_run = l_run * alpha + (ps[0] + ps[1]);
-    m_run = m_new;
+    l_run += ps[0] + ps[1];
     if constexpr (WEIGHTED) {
-      record_block(a, b, j0 + i0, g * G + col, ps[0], m_new, kgrp == 0 && col < G);
-      record_block(a, b, j0 + i1, g * G + col, ps[1], m_new, kgrp == 1 && col < G && i1 >= 0);
+      // k-group 0 ends up with the first block's sum, k-group 1 with the second's
+      const int i = kgrp == 0 ? i0 : i1;
+      const float sum = sum_kgroups2(ps[0], ps[1]);
+      if (kgrp < 2 && col < G && i >= 0) bl[i * G] = m_run + __log2f(sum);
     }
     u32x2 va[VT], vb[VT];
     unpack_v<D>(R.v[0], R.vs[0], va);
     unpack_v<D>(R.v[1], R.vs[1], vb);
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      acc[t] *= alpha;
+    for (int t = 0; t < VT; ++t)
       acc[t] = mfma16x16x32(as_bf16x8(u32x4{va[t].x, va[t].y, vb[t].x, vb[t].y}), as_bf16x8(pf),
                             acc[t]);
-    }
   };
 
   // ring of DEPTH pairs: DEPTH-1 pairs load while one computes
@@ -470,7 +462,10 @@ extern "C" local_status_t local_paged_attn_decode_kv4(
   a.Hkv = Hkv;
   a.group = Hq / Hkv;
   a.max_blocks = max_blocks;
-  a.scale_log2 = sm_scale * kLog2e;
+  const Scale4 scale = scale_of(sm_scale);
+  a.scale_log2 = scale.log2;
+  a.q_xor = scale.q_xor;
+  a.q_and = scale.q_and;
   const DecodeParts part = decode_parts(a, B, D, true);
   // (the same with and without weights, so that one query serves both)
   const size_t need = align256(part.bytes) + block_lse_bytes(B, Hq, max_blocks);
