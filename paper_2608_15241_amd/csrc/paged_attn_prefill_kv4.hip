@@ -61,9 +61,8 @@ struct Prefill4Args {
   uint16_t* out;
   float* lse;
   // workspace
-  int* counts;     // units of the plan, tiles
-  int4* plan;      // units, longest first: request, tile, range, ranges of the tile
-  int4* tiles;     // request, tile, blocks that its last row sees, ranges
+  int4* plan;      // units (Unit4), longest first, then ones of no request
+  int4* tiles;     // first token, first row, rows, ranges; then ones of no rows
   float* part_o;   // [T][Hq][ranges][D]
   float* part_ml;  // [T][Hq][ranges][2]
   int64_t T, num_blocks;
@@ -78,24 +77,19 @@ __device__ __forceinline__ bool rows_ok4(int r0, int r1, int64_t T) {
   return r0 >= 0 && r1 >= r0 && r1 <= T;
 }
 
-// What a workgroup has to know of its tile of 128 rows.
-struct Tile4 {
-  int b, r0, row0, rows;   // request, its first token, first row of the tile, its rows
-  int prefix;              // cached tokens before the chunk
-  int blocks;              // blocks that the tile's last row sees
+// A unit of work: a tile of 128 rows of a request, or a range of its keys.
+struct Unit4 {
+  int b, range, n_ranges, r0;     // request (-1: none), range of so many, first token
+  int row0, rows, prefix, lo;     // first row and rows, cached tokens, blocks [lo, hi)
+  int hi, L, rv, none;            // context length and version of the request
 };
+constexpr int kUnitInt4s = sizeof(Unit4) / sizeof(int4);
 
-__device__ __forceinline__ Tile4 tile_of(const Prefill4Args& a, int b, int tile) {
-  Tile4 t;
-  t.b = b;
-  t.r0 = a.q_indptr[b];
-  const int n = a.q_indptr[b + 1] - t.r0, L = a.ctx_lens[b];
-  t.row0 = tile * kP4Rows;
-  t.rows = min(kP4Rows, n * a.group - t.row0);
-  t.prefix = L - n;
-  const int last = t.prefix + (t.row0 + t.rows - 1) / a.group;  // its position
-  t.blocks = last < 0 ? 0 : min(last / kBlockSize + 1, a.max_blocks);
-  return t;
+// Blocks that the tile at row0 of a chunk of n tokens sees with its last row.
+__device__ __forceinline__ int blocks_of(const Prefill4Args& a, int n, int L, int row0) {
+  const int rows = min(kP4Rows, n * a.group - row0);
+  const int last = L - n + (row0 + rows - 1) / a.group;  // its position
+  return last < 0 ? 0 : min(last / kBlockSize + 1, a.max_blocks);
 }
 
 // Inclusive prefix sum over the append launch's workgroup.
@@ -116,12 +110,16 @@ __device__ __forceinline__ int scan_ap(int v, int* wave_sums) {
 // ---------------------------------------------------------------- plan
 // One workgroup. Units are ordered by a counting sort of their lengths in 256 steps
 // (the order among equals does not matter to any result).
+constexpr int kPlanCache = 1024;  // tiles whose entries stay in LDS
+
 __device__ void plan_kv4(const Prefill4Args& a) {
+  __shared__ int4 cache[kPlanCache];
   __shared__ int first[kApThreads + 1], wave_sums[kApWaves], hist[256], longest;
   __shared__ unsigned long long work;
   const int tid = threadIdx.x;
   int n_tiles = 0;
   if (tid == 0) work = 0ull, longest = 1;
+  hist[tid] = 0;
   for (int b0 = 0; b0 < a.B; b0 += kApThreads) {
     int n = 0;
     if (b0 + tid < a.B) {
@@ -143,8 +141,13 @@ __device__ void plan_kv4(const Prefill4Args& a) {
         else
           hi = mid;
       }
-      const int tile = t - first[lo], blocks = tile_of(a, b0 + lo, tile).blocks;
-      a.tiles[n_tiles + t] = int4{b0 + lo, tile, blocks, 1};
+      const int b = b0 + lo, row0 = (t - first[lo]) * kP4Rows, at = n_tiles + t;
+      const int blocks = blocks_of(a, a.q_indptr[b + 1] - a.q_indptr[b], a.ctx_lens[b], row0);
+      const int4 e = {b, row0, blocks, 0};
+      if (at < kPlanCache)
+        cache[at] = e;
+      else
+        a.tiles[at] = e;
       atomicAdd(&work, static_cast<unsigned long long>(blocks));
       atomicMax(&longest, blocks);
     }
@@ -152,8 +155,6 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     __syncthreads();
   }
   // No unit longer than a compute unit's share of the work.
-  hist[tid] = 0;
-  __syncthreads();
   const int64_t share = (static_cast<int64_t>(work) * a.Hkv + kP4Units - 1) / kP4Units;
   auto ranges_of = [&](int blocks) {
     const int64_t want = (blocks + share - 1) / max(share, static_cast<int64_t>(1));
@@ -164,26 +165,40 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     return 255 - static_cast<int>(static_cast<int64_t>(blocks) * 255 /
                                   (static_cast<int64_t>(longest) * n));
   };
-  // (tile t of a.tiles is read by the thread that wrote it or after a barrier)
+  auto entry = [&](int t) { return t < kPlanCache ? cache[t] : a.tiles[t]; };
   for (int t = tid; t < n_tiles; t += kApThreads) {
-    const int blocks = a.tiles[t].z, n = ranges_of(blocks);
+    const int blocks = entry(t).z, n = ranges_of(blocks);
     atomicAdd(&hist[bucket(blocks, n)], n);
   }
   __syncthreads();
   const int mine = hist[tid], incl = scan_ap(mine, wave_sums);
-  if (tid == kApThreads - 1) {
-    a.counts[0] = incl;
-    a.counts[1] = n_tiles;
-  }
-  hist[tid] = incl - mine;
+  const int before = incl - mine;
   __syncthreads();
-  for (int t = tid; t < n_tiles; t += kApThreads) {
-    const int4 e = a.tiles[t];
-    const int n = ranges_of(e.z);
-    a.tiles[t].w = n;
-    const int at = atomicAdd(&hist[bucket(e.z, n)], n);
-    for (int r = 0; r < n; ++r) a.plan[at + r] = int4{e.x, e.y, r, n};
+  hist[tid] = before;
+  if (tid == kApThreads - 1) first[0] = incl;
+  __syncthreads();
+  const int units = first[0];
+  for (int t = tid; t < a.max_tiles; t += kApThreads) {
+    if (t >= n_tiles) {
+      a.tiles[t] = int4{0, 0, 0, 1};
+      continue;
+    }
+    const int4 e = entry(t);
+    const int b = e.x, row0 = e.y, blocks = e.z, n = ranges_of(blocks);
+    const int r0 = a.q_indptr[b], tokens = a.q_indptr[b + 1] - r0, L = a.ctx_lens[b];
+    const int rows = min(kP4Rows, tokens * a.group - row0), rv = a.req_version[b];
+    a.tiles[t] = int4{r0, row0, rows, n};
+    const int at = atomicAdd(&hist[bucket(blocks, n)], n);
+    for (int r = 0; r < n; ++r) {
+      int4* u = a.plan + static_cast<int64_t>(at + r) * kUnitInt4s;
+      u[0] = int4{b, r, n, r0};
+      u[1] = int4{row0, rows, L - tokens,
+                  static_cast<int>(static_cast<int64_t>(blocks) * r / n)};
+      u[2] = int4{static_cast<int>(static_cast<int64_t>(blocks) * (r + 1) / n), L, rv, 0};
+    }
   }
+  for (int u = units + tid; u < a.max_tiles * a.ranges; u += kApThreads)
+    a.plan[static_cast<int64_t>(u) * kUnitInt4s] = int4{-1, 0, 0, 0};
 }
 
 // ---------------------------------------------------------------- append
@@ -245,49 +260,55 @@ __global__ __launch_bounds__(kApThreads) void append_kv4_kernel(Prefill4Args a) 
     return (static_cast<int64_t>(r0 + slot + off) * a.Hkv + g) * D;
   };
   uint8_t* o = a.kv4 + (static_cast<int64_t>(p) * a.Hkv + g) * L4::kTile;
-  // K: slot col, dims (D/4) kgrp ..; V: slots 4 kgrp .., dims VT col ..
-  u32x4 kv[D / 32];
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    kv[c] = u32x4{0u, 0u, 0u, 0u};
-    if (fresh(col)) kv[c] = ld_global<u32x4>(a.k_new + row(col) + (D / 4) * kgrp + 8 * c);
-  }
-  u32x4 vv[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    vv[e] = u32x4{0u, 0u, 0u, 0u};
+  // A lane takes the same dims of K and V, VT col .., of slots 4 kgrp .. (whole rows are
+  // read side by side; K by the lane that holds its codes in attention read 64 places).
+  auto read = [&](const uint16_t* x, int e) {
+    u32x4 v = {0u, 0u, 0u, 0u};
     if (fresh(4 * kgrp + e)) {
-      const uint16_t* from = a.v_new + row(4 * kgrp + e) + VT * col;
+      const uint16_t* from = x + row(4 * kgrp + e) + VT * col;
       if constexpr (D == 128) {
-        vv[e] = ld_global<u32x4>(from);
+        v = ld_global<u32x4>(from);
       } else {
         const u32x2 w = ld_global<u32x2>(from);
-        vv[e] = u32x4{w.x, w.y, 0u, 0u};
+        v = u32x4{w.x, w.y, 0u, 0u};
       }
     }
-  }
-  uint32_t code[D / 32], vcode[4], vs[4];
-  const uint32_t ks = round_k<D>(kv, code);
+    return v;
+  };
+  u32x4 kv[4], vv[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) vs[e] = round_v<D>(vv[e], vcode[e]);
-  if (fresh(col)) {
-    uint32_t* to = reinterpret_cast<uint32_t*>(o + lane * L4::kLane);
+  for (int e = 0; e < 4; ++e) kv[e] = read(a.k_new, e), vv[e] = read(a.v_new, e);
+  uint32_t kcode[4], ks[4], vcode[4], vs[4];
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) to[c] = code[c];
-    if (D == 128 || kgrp % 2 == 0)
-      o[L4::k_scale(L4::k_group(kgrp), col)] = static_cast<uint8_t>(ks);
+  for (int e = 0; e < 4; ++e) {
+    ks[e] = round_v<D>(kv[e], kcode[e]);
+    vs[e] = round_v<D>(vv[e], vcode[e]);
   }
+  const int d = VT * col, group = L4::v_group(col);
+  const bool head = col % (16 / L4::kGroups) == 0;  // of the group's lanes
   uint8_t* vo = o + L4::kV + lane * L4::kLane;
-  const bool head = col % (16 / L4::kGroups) == 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int s = 4 * kgrp + e;
+    if (!fresh(s)) continue;
+    uint8_t* ko = o + (d / (D / 4) * kBlockSize + s) * L4::kLane + d % (D / 4) / 2;
+    if constexpr (D == 128)
+      *reinterpret_cast<uint32_t*>(ko) = kcode[e];
+    else
+      *reinterpret_cast<uint16_t*>(ko) = static_cast<uint16_t>(kcode[e]);
+  }
   if (fresh(4 * kgrp) && fresh(4 * kgrp + 3)) {  // the lane's four slots at once
     if constexpr (D == 128)
       *reinterpret_cast<u32x4*>(vo) = u32x4{vcode[0], vcode[1], vcode[2], vcode[3]};
     else
       *reinterpret_cast<u32x2*>(vo) = u32x2{(vcode[0] & 0xffffu) | vcode[1] << 16,
                                             (vcode[2] & 0xffffu) | vcode[3] << 16};
-    if (head)
-      *reinterpret_cast<uint32_t*>(o + L4::v_scale(L4::v_group(col), 4 * kgrp)) =
+    if (head) {
+      *reinterpret_cast<uint32_t*>(o + L4::k_scale(group, 4 * kgrp)) =
+          ks[0] | ks[1] << 8 | ks[2] << 16 | ks[3] << 24;
+      *reinterpret_cast<uint32_t*>(o + L4::v_scale(group, 4 * kgrp)) =
           vs[0] | vs[1] << 8 | vs[2] << 16 | vs[3] << 24;
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -296,8 +317,10 @@ __global__ __launch_bounds__(kApThreads) void append_kv4_kernel(Prefill4Args a) 
         reinterpret_cast<uint32_t*>(vo)[e] = vcode[e];
       else
         reinterpret_cast<uint16_t*>(vo)[e] = static_cast<uint16_t>(vcode[e]);
-      if (head)
-        o[L4::v_scale(L4::v_group(col), 4 * kgrp + e)] = static_cast<uint8_t>(vs[e]);
+      if (head) {
+        o[L4::k_scale(group, 4 * kgrp + e)] = static_cast<uint8_t>(ks[e]);
+        o[L4::v_scale(group, 4 * kgrp + e)] = static_cast<uint8_t>(vs[e]);
+      }
     }
   }
 }
@@ -335,69 +358,99 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   using L4 = Kv4<D>;
   constexpr int KC = D / 32, VT = D / 16, RT = kP4RowTiles;
   __shared__ Stage4<D> stage[kP4Halves][2];
+
   __shared__ __attribute__((aligned(16))) int list_id[kP4Window + 2 * kP4Step],
       list_j[kP4Window + 2 * kP4Step];
   __shared__ int wave_n[kP4Halves * kP4Waves];
-  static_assert(sizeof(stage) >= kP4Rows * (D + 4 + 2) * sizeof(float), "joins in the stages");
+  static_assert(sizeof(stage) >= kP4Rows * (D + 4 + 2) * sizeof(float), "joined in the stages");
 
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave_all = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int wave = wave_all % kP4Waves, half = wave_all / kP4Waves;
   const int col = lane % 16, kgrp = lane / 16;
-  const int g = blockIdx.x % a.Hkv;
-  const int slot = blockIdx.x / a.Hkv;
-  if (slot >= a.counts[0]) return;
-  const int4 unit = a.plan[slot];
-  const int b = unit.x, range = unit.z, n_ranges = unit.w;
-  const Tile4 tl = tile_of(a, b, unit.y);
-  const int lo = static_cast<int>(static_cast<int64_t>(tl.blocks) * range / n_ranges);
-  const int hi = static_cast<int>(static_cast<int64_t>(tl.blocks) * (range + 1) / n_ranges);
-  const int L = a.ctx_lens[b], rv = a.req_version[b];
-  const int32_t* table = a.block_table + static_cast<int64_t>(b) * a.max_blocks;
+  // Unit p * gridDim + i of pass p, by falling length, every other pass the other way
+  // round (in steps of 8 workgroups, the XCDs: a KV head's units stay on one).
+  const uint32_t units = static_cast<uint32_t>(a.max_tiles) * a.ranges * a.Hkv;
+  auto unit_of = [&](uint32_t pass) {  // (below 2^31 + 256: the host checks)
+    const uint32_t i = blockIdx.x, n = gridDim.x;
+    const uint32_t turned = n % 8 == 0 ? (n / 8 - 1 - i / 8) * 8 + i % 8 : n - 1 - i;
+    return pass * n + (pass % 2 ? turned : i);
+  };
+  auto read_unit = [&](uint32_t u) {
+    Unit4 e;
+    e.b = -1;
+    if (u < units) {
+      // (read-only here and the same for the workgroup: scalar loads)
+      typedef const __attribute__((address_space(4))) u32x4* ScalarPtr;
+      const ScalarPtr from = (ScalarPtr)(a.plan + static_cast<int64_t>(u / static_cast<uint32_t>(a.Hkv)) * kUnitInt4s);
+      u32x4 w[kUnitInt4s];
+#pragma unroll
+      for (int i = 0; i < kUnitInt4s; ++i) w[i] = from[i];
+      __builtin_memcpy(&e, w, sizeof e);
+    }
+    return e;
+  };
+  // A table entry where it names a block of the pool, else -1; then with its tag.
+  auto read_id = [&](const Unit4& e, int j) {
+    const int p = j < e.hi ? a.block_table[static_cast<int64_t>(e.b) * a.max_blocks + j] : -1;
+    return p >= 0 && p < a.num_blocks ? p : -1;
+  };
+  auto read_tag = [&](int p) { return p >= 0 ? a.block_version[p] : 0; };
+
+  uint32_t pass = 0;
+  Unit4 e = read_unit(unit_of(0));
+  if (e.b < 0) return;
+  int g = static_cast<int>(unit_of(0) % static_cast<uint32_t>(a.Hkv));
+  int id = read_id(e, e.lo + tid);
+  if (read_tag(id) != e.rv) id = -1;
 
   // This wave's rows: column col of row tile r is row 32 wave + 16 r + col of the tile.
-  int pos[RT];        // its position, -1 for none
-  int64_t qrow[RT];   // token * Hq + head
-  bf16x8 qv[RT][KC];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
+  auto row_of = [&](const Unit4& u, int head, int r, int* position) {
     const int row = 16 * RT * wave + 16 * r + col;
-    const bool in = row < tl.rows;
-    const int at = tl.row0 + (in ? row : 0);
+    const bool in = row < u.rows;
+    const int at = u.row0 + (in ? row : 0);
     const int i = at / a.group;
-    pos[r] = in ? tl.prefix + i : -1;
-    qrow[r] = static_cast<int64_t>(tl.r0 + i) * a.Hq + g * a.group + at % a.group;
+    *position = in ? u.prefix + i : -1;
+    return static_cast<int64_t>(u.r0 + i) * a.Hq + head * a.group + at % a.group;
+  };
+  int pos[RT];  // a row's position, -1 for none
+  bf16x8 qv[RT][KC];
+  auto read_q = [&](const Unit4& u, int head) {
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      u32x4 v = {0u, 0u, 0u, 0u};
-      if (in) v = ld_global<u32x4>(a.q + qrow[r] * D + (D / 4) * kgrp + 8 * c);
-      qv[r][c] = as_bf16x8((v ^ a.q_xor) & a.q_and);
+    for (int r = 0; r < RT; ++r) {
+      const int64_t row = row_of(u, head, r, &pos[r]);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (pos[r] != -1 || 16 * RT * wave + 16 * r + col < u.rows)
+          v = ld_global<u32x4>(a.q + row * D + (D / 4) * kgrp + 8 * c);
+        qv[r][c] = as_bf16x8((v ^ a.q_xor) & a.q_and);
+      }
     }
-  }
-  // Positions of the wave's first and last row: bounds of what it may see.
-  const int wrow = tl.row0 + 16 * RT * wave;
-  const bool wave_in = 16 * RT * wave < tl.rows, wave_full = 16 * RT * (wave + 1) <= tl.rows;
-  const int first_pos = tl.prefix + wrow / a.group;
-  const int last_pos =
-      wave_in ? tl.prefix + (min(wrow + 16 * RT, tl.row0 + tl.rows) - 1) / a.group : -1;
+  };
+  read_q(e, g);
 
   f32x4 acc[RT][VT];
   float m_run[RT], l_run[RT], rise[RT];
   const float inv_scale = 1.f / a.scale_log2;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    m_run[r] = kP4NegBig;
-    l_run[r] = 0.f;
-    rise[r] = (kP4NegBig + kP4Lazy) * inv_scale;
-#pragma unroll
-    for (int t = 0; t < VT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  // Positions of the wave's first and last row: bounds of what it may see.
+  bool wave_full = false;
+  int first_pos = 0, last_pos = -1;
 
+  // Lane i holds what the half's i-th step of a window takes: its blocks' logical
+  // indices and the id of the one that this wave unpacks.
+  static_assert(kP4Window == kWave * kP4Halves * kP4Step, "a lane a step");
+  int my_id = -1;
+  int4 my_j4 = {0, 0, 0, 0};
+  auto j_of = [&](int s, int e) {
+    return __builtin_amdgcn_readlane(e == 0 ? my_j4.x : e == 1 ? my_j4.y : e == 2 ? my_j4.z
+                                                                                : my_j4.w, s);
+  };
   // This wave unpacks block `wave` of its half's steps.
   auto load = [&](Codes4<D>& c, int s) {
-    const int id = __builtin_amdgcn_readfirstlane(list_id[kP4Step * s + wave]);
-    const int64_t tile = (static_cast<int64_t>(max(id, 0)) * a.Hkv + g) * L4::kTile;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.kv4 + tile, id >= 0 ? L4::kTile : 0u);
+    const int p = __builtin_amdgcn_readlane(my_id, s);
+    const int64_t tile = (static_cast<int64_t>(max(p, 0)) * a.Hkv + g) * L4::kTile;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.kv4 + tile, p >= 0 ? L4::kTile : 0u);
     load_cached<D>(r, lane * L4::kLane, c.k);
     load_cached<D>(r, L4::kV + lane * L4::kLane, c.v);
     c.ks = __builtin_amdgcn_raw_buffer_load_b8(r, L4::k_scale(L4::k_group(kgrp), col), 0, 0);
@@ -410,13 +463,13 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
       st.k[wave][i][lane] = u32x4{unpack4<0>(c.k[i], ks), unpack4<1>(c.k[i], ks),
                                   unpack4<2>(c.k[i], ks), unpack4<3>(c.k[i], ks)};
     // V: slots past the context's end, and tokens that are not finite, as zeros
-    const int j = __builtin_amdgcn_readfirstlane(list_j[kP4Step * s + wave]);
-    const bool last = L - j * kBlockSize < kBlockSize;
+    const int j = j_of(s, wave);
+    const bool last = e.L - j * kBlockSize < kBlockSize;
     // (a byte of 255 is a zero byte of the complement)
     const bool bad = ((~c.vs - 0x01010101u) & c.vs & 0x80808080u) != 0u;
     uint32_t odd = 0u;
     if (last || __ballot(bad)) {
-      const int live = L - j * kBlockSize - 4 * kgrp;  // (no block: far below 0)
+      const int live = e.L - j * kBlockSize - 4 * kgrp;  // (no block: far below 0)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t byte = 0xffu << (8 * i);
@@ -446,22 +499,41 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
     int j[kP4Step];
 #pragma unroll
     for (int e = 0; e < kP4Step; ++e)
-      j[e] = __builtin_amdgcn_readfirstlane(list_j[kP4Step * s + e]);
+      j[e] = j_of(s, e);
     if (j[0] * kBlockSize > last_pos) return;  // (ascending: no key of the step is seen)
+    // Operands are read a block of K (half a pair of V) ahead of their products; left to
+    // itself the compiler reads two at a time and waits for each.
     f32x4 sc[RT][kP4Step];
+    u32x4 kf[2][KC];
+#pragma unroll
+    for (int c = 0; c < KC; ++c) kf[0][c] = st.k[0][c][lane];
 #pragma unroll
     for (int e = 0; e < kP4Step; ++e) {
+      if (e + 1 < kP4Step) {
+#pragma unroll
+        for (int c = 0; c < KC; ++c) kf[(e + 1) % 2][c] = st.k[e + 1][c][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < RT; ++r) sc[r][e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        const bf16x8 kf = as_bf16x8(st.k[e][c][lane]);
+      for (int c = 0; c < KC; ++c)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) sc[r][e] = mfma16x16x32(kf, qv[r][c], sc[r][e]);
-      }
+        for (int r = 0; r < RT; ++r)
+          sc[r][e] = mfma16x16x32(as_bf16x8(kf[e % 2][c]), qv[r][c], sc[r][e]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    constexpr int VG = VT / 2, kGroups = kP4Step / 2 * 2;  // groups of V tiles
+    u32x4 vf[2][VG];
+    auto read_v = [&](int q) {
+#pragma unroll
+      for (int t = 0; t < VG; ++t)
+        vf[q % 2][t] = *reinterpret_cast<const u32x4*>(&st.v[q / 2][q % 2 * VG + t][lane][0]);
+    };
+    read_v(0);
     // Keys past a row's position (those of no block lie past every position).
     if (!wave_full || j[kP4Step - 1] * kBlockSize + kBlockSize - 1 > first_pos) {
+      asm volatile("");  // (a branch: as selects it costs every step 64 instructions)
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -505,15 +577,16 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
       l_run[r] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
 #pragma unroll
-    for (int pr = 0; pr < kP4Step / 2; ++pr)
+    for (int q = 0; q < kGroups; ++q) {
+      if (q + 1 < kGroups) read_v(q + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < VT; ++t) {
-        const bf16x8 vf =
-            as_bf16x8(*reinterpret_cast<const u32x4*>(&st.v[pr][t][lane][0]));
+      for (int t = 0; t < VG; ++t)
 #pragma unroll
         for (int r = 0; r < RT; ++r)
-          acc[r][t] = mfma16x16x32(vf, as_bf16x8(pf[r][pr]), acc[r][t]);
-      }
+          acc[r][q % 2 * VG + t] = mfma16x16x32(as_bf16x8(vf[q % 2][t]), as_bf16x8(pf[r][q / 2]),
+                                                acc[r][q % 2 * VG + t]);
+    }
     // Tokens whose V is not finite, in the rows that see them (a lane's dims all lie
     // in one group).
     uint32_t bad[kP4Step], any = 0u;
@@ -537,116 +610,197 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
     }
   };
 
-  for (int w0 = lo; w0 < hi; w0 += kP4Window) {
-    // the window's valid blocks, in ascending order
-    const int j = w0 + tid;
-    int id = -1;
-    if (j < hi) {
-      const int p = table[j];
-      if (p >= 0 && p < a.num_blocks && a.block_version[p] == rv) id = p;
-    }
-    const uint64_t m = __ballot(id >= 0);
+  // A window's valid blocks in ascending order: counted, then (behind a barrier) listed.
+  auto count_ids = [&](int p) {
+    const uint64_t m = __ballot(p >= 0);
     if (lane == 0) wave_n[wave_all] = __popcll(m);
-    __syncthreads();
+  };
+  auto list_ids = [&](int p, int j) {
+    const uint64_t m = __ballot(p >= 0);
     int before = 0, n = 0;
 #pragma unroll
     for (int w = 0; w < kP4Halves * kP4Waves; ++w) {
       before += w < wave_all ? wave_n[w] : 0;
       n += wave_n[w];
     }
-    if (id >= 0) {
+    if (p >= 0) {
       const int at = before + __popcll(m & ((1ull << lane) - 1ull));
-      list_id[at] = id;
+      list_id[at] = p;
       list_j[at] = j;
     }
     if (tid < 2 * kP4Step) {  // the rest of the halves' last steps: no block
       list_id[n + tid] = -1;
       list_j[n + tid] = (INT_MAX - kBlockSize) / kBlockSize;
     }
-    __syncthreads();
-    // step 2 i + half is this half's i-th
-    const int steps = (n + kP4Halves * kP4Step - 1) / (kP4Halves * kP4Step);
-    if (steps > 0) {
-      Codes4<D> c;
-      load(c, half);
-      unpack(c, stage[half][0], half);
-      if (steps > 1) load(c, kP4Halves + half);
-      __syncthreads();
-      for (int i = 0; i < steps; ++i) {
-        if (i + 1 < steps) {
-          unpack(c, stage[half][(i + 1) % 2], kP4Halves * (i + 1) + half);
-          if (i + 2 < steps) load(c, kP4Halves * (i + 2) + half);
-        }
-        compute(stage[half][i % 2], kP4Halves * i + half);
-        __syncthreads();
-      }
-    }
-    __syncthreads();  // (the list is written again)
-  }
+    return n;
+  };
 
-  // ---- finish: the rows' sums over the k-groups, the halves joined through LDS (the
-  // second writes, the first adds), then the outputs. A lane's dims are 4 * VT
-  // neighbours: (4 kgrp + i) * VT + t.
+  // The halves' results are joined through LDS: half h finishes row tile h of each wave
+  // pair, the other half hands its part over. A lane's dims are 4 * VT neighbours:
+  // (4 kgrp + i) * VT + t.
+  static_assert(RT == kP4Halves, "a row tile a half");
   constexpr int kRow = D + 4;
   float* join = reinterpret_cast<float*>(&stage[0][0]);
   float* join_ml = join + kP4Rows * kRow;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    l_run[r] += __shfl_xor(l_run[r], 16);
-    l_run[r] += __shfl_xor(l_run[r], 32);
-  }
-  if (half == 1) {
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int row = 16 * RT * wave + 16 * r + col;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t = 0; t < VT; t += 4)
-          *reinterpret_cast<f32x4*>(join + row * kRow + (4 * kgrp + i) * VT + t) =
-              f32x4{acc[r][t][i], acc[r][t + 1][i], acc[r][t + 2][i], acc[r][t + 3][i]};
-      if (kgrp == 0) {
-        join_ml[2 * row] = m_run[r];
-        join_ml[2 * row + 1] = l_run[r];
-      }
-    }
-  }
-  __syncthreads();
-  if (half == 1) return;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
+  auto hand_over = [&](const f32x4(&x)[VT], float m, float l, int r) {
     const int row = 16 * RT * wave + 16 * r + col;
-    if (row >= tl.rows) continue;
-    const float m1 = join_ml[2 * row], l1 = join_ml[2 * row + 1];
-    const float M = fmaxf(m_run[r], m1);
-    const float f0 = fast_exp2(m_run[r] - M), f1 = fast_exp2(m1 - M);
-    const float l = l_run[r] * f0 + l1 * f1;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int64_t at = qrow[r] * a.ranges + range;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int t = 0; t < VT; t += 4) {
-        const int d = (4 * kgrp + i) * VT + t;
-        const f32x4 o1 = *reinterpret_cast<const f32x4*>(join + row * kRow + d);
-        f32x4 o = {acc[r][t][i], acc[r][t + 1][i], acc[r][t + 2][i], acc[r][t + 3][i]};
-        o = o * f0 + o1 * f1;
-        if (n_ranges == 1) {
-          o *= inv;
-          *reinterpret_cast<u32x2*>(a.out + qrow[r] * D + d) =
-              u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+      for (int t = 0; t < VT; t += 4)
+        *reinterpret_cast<f32x4*>(join + row * kRow + (4 * kgrp + i) * VT + t) =
+            f32x4{x[t][i], x[t + 1][i], x[t + 2][i], x[t + 3][i]};
+    if (kgrp == 0) {
+      join_ml[2 * row] = m;
+      join_ml[2 * row + 1] = l;
+    }
+  };
+  auto finish = [&](const Unit4& u, int head, const f32x4(&x)[VT], float m, float l0, int r) {
+    const int row0 = 16 * RT * wave + 16 * r;  // of this wave's 16 rows
+    if (row0 >= u.rows) return;
+    int position;
+    const int64_t to = row_of(u, head, r, &position);
+    float* mine = join + (row0 + col) * kRow;
+    const float m1 = join_ml[2 * (row0 + col)], l1 = join_ml[2 * (row0 + col) + 1];
+    const float M = fmaxf(m, m1);
+    const float f0 = fast_exp2(m - M), f1 = fast_exp2(m1 - M);
+    const float l = l0 * f0 + l1 * f1;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    f32x4 o[4][VT / 4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < VT / 4; ++t) {
+        const f32x4 o1 = *reinterpret_cast<const f32x4*>(mine + (4 * kgrp + i) * VT + 4 * t);
+        o[i][t] = f32x4{x[4 * t][i], x[4 * t + 1][i], x[4 * t + 2][i], x[4 * t + 3][i]} * f0 +
+                  o1 * f1;
+      }
+    // The wave's rows go back into their places in LDS and out in whole rows: stored from
+    // here, 8 bytes a lane and row, they took 12 us of the 4 x 512 tokens' 81.
+    asm volatile("" ::: "memory");  // (each row's old contents are read by now)
+    const bool whole = u.n_ranges == 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < VT / 4; ++t) {
+        const int d = (4 * kgrp + i) * VT + 4 * t;
+        if (whole) {
+          const f32x4 v = o[i][t] * inv;
+          *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(mine) + d) =
+              u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
         } else {
-          *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = o;
+          *reinterpret_cast<f32x4*>(mine + d) = o[i][t];
         }
       }
-    if (kgrp == 0) {
-      if (n_ranges > 1) {
+    asm volatile("" ::: "memory");
+    const int per_row = whole ? D / 8 : D / 4;  // lanes of 16 bytes
+    for (int k = 0; k < per_row / 4; ++k) {
+      const int row = k * (kWave / per_row) + lane / per_row, piece = lane % per_row;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(
+          reinterpret_cast<const char*>(join + (row0 + row) * kRow) + 16 * piece);
+      const int64_t q = static_cast<int64_t>(__shfl(static_cast<long long>(to), row));
+      if (row0 + row < u.rows) {
+        if (whole)
+          *reinterpret_cast<u32x4*>(a.out + q * D + 8 * piece) = v;
+        else
+          *reinterpret_cast<u32x4*>(a.part_o + (q * a.ranges + u.range) * D + 4 * piece) = v;
+      }
+    }
+    if (kgrp == 0 && row0 + col < u.rows) {
+      if (!whole) {
+        const int64_t at = to * a.ranges + u.range;
         a.part_ml[2 * at] = M;
         a.part_ml[2 * at + 1] = l;
       } else if (a.lse) {
-        a.lse[qrow[r]] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
+        a.lse[to] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
       }
     }
+  };
+
+  // Units one after the other. What the next one starts from (its entry, its first
+  // window's ids and tags, q) is read while this one runs: a unit's chain of dependent
+  // loads took as long as a third of its steps.
+  count_ids(id);
+  __syncthreads();
+  int n = list_ids(id, e.lo + tid);
+  for (;;) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      m_run[r] = kP4NegBig;
+      l_run[r] = 0.f;
+      rise[r] = (kP4NegBig + kP4Lazy) * inv_scale;
+#pragma unroll
+      for (int t = 0; t < VT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int wrow = 16 * RT * wave;
+    wave_full = wrow + 16 * RT <= e.rows;
+    first_pos = e.prefix + (e.row0 + wrow) / a.group;
+    last_pos =
+        wrow < e.rows ? e.prefix + (e.row0 + min(wrow + 16 * RT, e.rows) - 1) / a.group : -1;
+    __syncthreads();
+
+    Unit4 next;
+    int next_id = -1, next_tag = 0;
+    for (int w0 = e.lo;;) {
+      // step 2 i + half is this half's i-th
+      const int steps = (n + kP4Halves * kP4Step - 1) / (kP4Halves * kP4Step);
+      const int mine = kP4Step * (kP4Halves * lane + half);  // (lanes past `steps`: unused)
+      my_id = list_id[mine + wave];
+      my_j4 = *reinterpret_cast<const int4*>(&list_j[mine]);
+      Codes4<D> c;
+      if (steps > 0) load(c, 0);
+      const bool start = w0 == e.lo;
+      if (start) {
+        next = read_unit(unit_of(pass + 1));
+        if (next.b >= 0) next_id = read_id(next, next.lo + tid);
+      }
+      if (steps > 0) unpack(c, stage[half][0], 0);
+      if (start && next.b >= 0) next_tag = read_tag(next_id);
+      if (steps > 1) load(c, 1);
+      __syncthreads();
+      for (int i = 0; i < steps; ++i) {
+        if (i + 1 < steps) {
+          unpack(c, stage[half][(i + 1) % 2], i + 1);
+          if (i + 2 < steps) load(c, i + 2);
+        }
+        compute(stage[half][i % 2], i);
+        __syncthreads();
+      }
+      w0 += kP4Window;
+      if (w0 >= e.hi) break;
+      int p = read_id(e, w0 + tid);
+      if (read_tag(p) != e.rv) p = -1;
+      count_ids(p);
+      __syncthreads();
+      n = list_ids(p, w0 + tid);
+      __syncthreads();
+    }
+
+    const int next_g = static_cast<int>(unit_of(pass + 1) % static_cast<uint32_t>(a.Hkv));
+    if (next.b >= 0) {
+      read_q(next, next_g);
+      id = next_tag == next.rv ? next_id : -1;
+      count_ids(id);
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      l_run[r] += __shfl_xor(l_run[r], 16);
+      l_run[r] += __shfl_xor(l_run[r], 32);
+    }
+    if (half == 0)
+      hand_over(acc[1], m_run[1], l_run[1], 1);
+    else
+      hand_over(acc[0], m_run[0], l_run[0], 0);
+    __syncthreads();
+    if (half == 0)
+      finish(e, g, acc[0], m_run[0], l_run[0], 0);
+    else
+      finish(e, g, acc[1], m_run[1], l_run[1], 1);
+    if (next.b < 0) return;
+    n = list_ids(id, next.lo + tid);
+    e = next;
+    g = next_g;
+    ++pass;
   }
 }
 
@@ -658,17 +812,14 @@ template <int D>
 __global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
   const int g = blockIdx.x % a.Hkv;
   const int rest = blockIdx.x / a.Hkv;
-  if (rest / 4 >= a.counts[1]) return;
   const int4 e = a.tiles[rest / 4];
-  const int n = e.w;
+  const int r0 = e.x, row0 = e.y, rows = e.z, n = e.w;
   if (n == 1) return;
-  const Tile4 tl = tile_of(a, e.x, e.y);
   for (int x = threadIdx.x; x < kMgRows * (D / 4); x += kApThreads) {
     const int row = rest % 4 * kMgRows + x / (D / 4), d = 4 * (x % (D / 4));
-    if (row >= tl.rows) break;
-    const int at = tl.row0 + row;
-    const int64_t q =
-        static_cast<int64_t>(tl.r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
+    if (row >= rows) break;
+    const int at = row0 + row;
+    const int64_t q = static_cast<int64_t>(r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml + q * a.ranges * 2);
     const float* po = a.part_o + q * a.ranges * D + d;
     float M = kP4NegBig, den = 0.f;
@@ -689,14 +840,15 @@ __global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
 template <int D>
 local_status_t launch_prefill_kv4(const Prefill4Args& a, hipStream_t s) {
   const char* who = "paged_attn_prefill_kv4";
-  const int64_t grid = static_cast<int64_t>(a.max_tiles) * a.ranges * a.Hkv;
+  const int64_t units = static_cast<int64_t>(a.max_tiles) * a.ranges * a.Hkv;
+  const int64_t grid = std::min<int64_t>(units, kP4Units);
   // blocks that hold a chunk's tokens: at most one more than the chunk fills, each side
   const int64_t blocks = a.T / kBlockSize + 2 * static_cast<int64_t>(a.B);
   const int64_t append = 1 + (blocks * a.Hkv + kApWaves - 1) / kApWaves;
   const int64_t merge = a.ranges > 1 ? static_cast<int64_t>(a.max_tiles) * 4 * a.Hkv : 0;
-  if (grid >= (1LL << 31) || append >= (1LL << 31) || merge >= (1LL << 31))
-    return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: grids of %lld, %lld and %lld workgroups", who,
-                      (long long)grid, (long long)append, (long long)merge);
+  if (units >= (1LL << 31) || append >= (1LL << 31) || merge >= (1LL << 31))
+    return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: %lld units, grids of %lld and %lld workgroups",
+                      who, (long long)units, (long long)append, (long long)merge);
   if (a.k_new)
     append_kv4_kernel<D><<<static_cast<unsigned>(append), kApThreads, 0, s>>>(a);
   else
@@ -747,7 +899,7 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   a.max_tiles = static_cast<int>(tiles);
   a.ranges = B > 0 && T > 0 ? ranges_of_call(tiles, Hkv, max_blocks) : 1;
   const size_t rows = static_cast<size_t>(T) * Hq * (a.ranges > 1 ? a.ranges : 0);
-  const size_t plan_at = 256, tiles_at = plan_at + sizeof(int4) * tiles * a.ranges;
+  const size_t tiles_at = sizeof(Unit4) * tiles * a.ranges;
   const size_t part_at = round256(tiles_at + sizeof(int4) * tiles);
   const size_t need = part_at + rows * (D + 2) * sizeof(float);
   if (!ws) {
@@ -776,8 +928,7 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   a.out = out;
   a.lse = lse;
   char* base = static_cast<char*>(ws);
-  a.counts = reinterpret_cast<int*>(base);
-  a.plan = reinterpret_cast<int4*>(base + plan_at);
+  a.plan = reinterpret_cast<int4*>(base);
   a.tiles = reinterpret_cast<int4*>(base + tiles_at);
   a.part_o = reinterpret_cast<float*>(base + part_at);
   a.part_ml = a.part_o + rows * D;

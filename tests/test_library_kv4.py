@@ -75,13 +75,13 @@ def test_workspace_sizes(lib):
     assert lib.local_paged_attn_decode(*plain, None, ctypes.byref(m), None) == OK
     assert n.value == (m.value + 255) // 256 * 256 + 4 * 64 * 32 * 4
     # few tiles of 128 rows (400 / 128 + 4 requests): up to 8 key ranges of at least 8
-    # blocks, (D + 2) floats a row and range, behind 16 bytes a unit and a tile
+    # blocks, (D + 2) floats a row and range, behind 48 bytes a unit and 16 a tile
     a = lambda v: (v + 255) // 256 * 256  # noqa: E731
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4), None, ctypes.byref(n), None) == OK
-    assert n.value == a(256 + 16 * 7 * 8 + 16 * 7) + 100 * 32 * 8 * 130 * 4
+    assert n.value == a(48 * 7 * 8 + 16 * 7) + 100 * 32 * 8 * 130 * 4
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, T=1 << 20), None, ctypes.byref(n),
                                             None) == OK
-    assert n.value == a(256 + 32 * ((1 << 15) + 4))
+    assert n.value == a(64 * ((1 << 15) + 4))
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, T=1 << 30), None, ctypes.byref(n),
                                             None) == ERR_UNSUPPORTED
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, T=-1), None, ctypes.byref(n),
