@@ -111,15 +111,18 @@ __device__ __forceinline__ int scan_ap(int v, int* wave_sums) {
 // One workgroup. Units are ordered by a counting sort of their lengths in 256 steps
 // (the order among equals does not matter to any result).
 constexpr int kPlanCache = 1024;  // tiles whose entries stay in LDS
+constexpr int kPlanChoices = 3;
 
 __device__ void plan_kv4(const Prefill4Args& a) {
   __shared__ int4 cache[kPlanCache];
   __shared__ int first[kApThreads + 1], wave_sums[kApWaves], hist[256], longest;
+  __shared__ int n_units[kPlanChoices];
   __shared__ unsigned long long work;
   const int tid = threadIdx.x;
   int n_tiles = 0;
   if (tid == 0) work = 0ull, longest = 1;
   hist[tid] = 0;
+  if (tid < kPlanChoices) n_units[tid] = 0;
   for (int b0 = 0; b0 < a.B; b0 += kApThreads) {
     int n = 0;
     if (b0 + tid < a.B) {
@@ -154,20 +157,42 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     n_tiles = min(n_tiles + all, a.max_tiles);
     __syncthreads();
   }
-  // No unit longer than a compute unit's share of the work.
-  const int64_t share = (static_cast<int64_t>(work) * a.Hkv + kP4Units - 1) / kP4Units;
-  auto ranges_of = [&](int blocks) {
-    const int64_t want = (blocks + share - 1) / max(share, static_cast<int64_t>(1));
-    const int most = min(a.ranges, blocks / kP4MinRange);
-    return static_cast<int>(max(static_cast<int64_t>(1), min(want, static_cast<int64_t>(most))));
+  // No unit longer than a compute unit's share of the work, or an eighth or a quarter
+  // more where that leaves no compute unit a second one (4 requests of 1 to 16 tokens behind 1K
+  // to 8K have units of one length: the share alone makes 270 of them, two rounds).
+  const float share = fmaxf(static_cast<float>(work) * a.Hkv / kP4Units, 1.f);
+  auto ranges_of = [&](int blocks, float inv_len) {
+    const int want = static_cast<int>(static_cast<float>(blocks) * inv_len + 0.999f);
+    return max(1, min(want, min(a.ranges, blocks / kP4MinRange)));
   };
   auto bucket = [&](int blocks, int n) {
-    return 255 - static_cast<int>(static_cast<int64_t>(blocks) * 255 /
-                                  (static_cast<int64_t>(longest) * n));
+    const float part = static_cast<float>(blocks) / (static_cast<float>(longest) * n);
+    return 255 - min(255, static_cast<int>(part * 255.f));
   };
   auto entry = [&](int t) { return t < kPlanCache ? cache[t] : a.tiles[t]; };
+  float inv_len = 1.f / share;
+  if (a.ranges > 1) {
+    constexpr float kLonger[kPlanChoices] = {1.f, 1.125f, 1.25f};
+    int n[kPlanChoices] = {0, 0, 0};
+    for (int t = tid; t < n_tiles; t += kApThreads) {
+      const int blocks = entry(t).z;
+#pragma unroll
+      for (int c = 0; c < kPlanChoices; ++c) n[c] += ranges_of(blocks, inv_len / kLonger[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < kPlanChoices; ++c) {
+#pragma unroll
+      for (int off = kWave / 2; off > 0; off >>= 1) n[c] += __shfl_xor(n[c], off);
+      if (tid % kWave == 0) atomicAdd(&n_units[c], n[c]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = kPlanChoices - 1; c >= 0; --c)
+      if (static_cast<int64_t>(n_units[c]) * a.Hkv <= kP4Units)
+        inv_len = 1.f / (share * kLonger[c]);
+  }
   for (int t = tid; t < n_tiles; t += kApThreads) {
-    const int blocks = entry(t).z, n = ranges_of(blocks);
+    const int blocks = entry(t).z, n = ranges_of(blocks, inv_len);
     atomicAdd(&hist[bucket(blocks, n)], n);
   }
   __syncthreads();
@@ -184,7 +209,7 @@ __device__ void plan_kv4(const Prefill4Args& a) {
       continue;
     }
     const int4 e = entry(t);
-    const int b = e.x, row0 = e.y, blocks = e.z, n = ranges_of(blocks);
+    const int b = e.x, row0 = e.y, blocks = e.z, n = ranges_of(blocks, inv_len);
     const int r0 = a.q_indptr[b], tokens = a.q_indptr[b + 1] - r0, L = a.ctx_lens[b];
     const int rows = min(kP4Rows, tokens * a.group - row0), rv = a.req_version[b];
     a.tiles[t] = int4{r0, row0, rows, n};
@@ -804,37 +829,57 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   }
 }
 
-// Joins the key ranges of the tiles that have more than one: a workgroup a quarter of a
-// tile and KV head, a thread 4 dims of a row.
-constexpr int kMgRows = kP4Rows / 4;
+// Joins the key ranges of the tiles that have more than one: a thread takes 4 dims of a
+// row, a workgroup the rows that its threads make.
+template <int D>
+constexpr int merge_rows() { return kApThreads / (D / 4); }
 
 template <int D>
 __global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
   const int g = blockIdx.x % a.Hkv;
   const int rest = blockIdx.x / a.Hkv;
-  const int4 e = a.tiles[rest / 4];
+  constexpr int kParts = kP4Rows / merge_rows<D>();
+  const int4 e = a.tiles[rest / kParts];
   const int r0 = e.x, row0 = e.y, rows = e.z, n = e.w;
-  if (n == 1) return;
-  for (int x = threadIdx.x; x < kMgRows * (D / 4); x += kApThreads) {
-    const int row = rest % 4 * kMgRows + x / (D / 4), d = 4 * (x % (D / 4));
-    if (row >= rows) break;
-    const int at = row0 + row;
-    const int64_t q = static_cast<int64_t>(r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
-    const float2* ml = reinterpret_cast<const float2*>(a.part_ml + q * a.ranges * 2);
-    const float* po = a.part_o + q * a.ranges * D + d;
-    float M = kP4NegBig, den = 0.f;
-    f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    for (int r = 0; r < n; ++r) M = fmaxf(M, ml[r].x);
-    for (int r = 0; r < n; ++r) {
-      const float f = fast_exp2(ml[r].x - M);
-      den += ml[r].y * f;
-      num += *reinterpret_cast<const f32x4*>(po + static_cast<int64_t>(r) * D) * f;
+  const int row = rest % kParts * merge_rows<D>() + threadIdx.x / (D / 4);
+  const int d = 4 * (threadIdx.x % (D / 4));
+  if (n == 1 || row >= rows) return;
+  const int at = row0 + row;
+  const int64_t q = static_cast<int64_t>(r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml + q * a.ranges * 2);
+  const float* po = a.part_o + q * a.ranges * D + d;
+  // every range's loads in flight at once, 8 at a time
+  constexpr int kBatch = 8;
+  float M = kP4NegBig, den = 0.f;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < n; p += kBatch) {
+    float2 m[kBatch];
+    f32x4 o[kBatch];
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) {
+      const int at_r = min(p + r, n - 1);
+      m[r] = ml[at_r];
+      o[r] = *reinterpret_cast<const f32x4*>(po + static_cast<int64_t>(at_r) * D);
     }
-    num *= den == 0.f ? 0.f : 1.f / den;
-    *reinterpret_cast<u32x2*>(a.out + q * D + d) =
-        u32x2{pack_bf16x2(num[0], num[1]), pack_bf16x2(num[2], num[3])};
-    if (d == 0 && a.lse) a.lse[q] = den == 0.f ? -INFINITY : (M + __log2f(den)) * kLn2;
+    float top = M;
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) top = fmaxf(top, m[r].x);
+    const float f = fast_exp2(M - top);
+    den *= f;
+    num *= f;
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) {
+      if (p + r >= n) break;
+      const float w = fast_exp2(m[r].x - top);
+      den += m[r].y * w;
+      num += o[r] * w;
+    }
+    M = top;
   }
+  num *= den == 0.f ? 0.f : 1.f / den;
+  *reinterpret_cast<u32x2*>(a.out + q * D + d) =
+      u32x2{pack_bf16x2(num[0], num[1]), pack_bf16x2(num[2], num[3])};
+  if (d == 0 && a.lse) a.lse[q] = den == 0.f ? -INFINITY : (M + __log2f(den)) * kLn2;
 }
 
 template <int D>
@@ -845,7 +890,7 @@ local_status_t launch_prefill_kv4(const Prefill4Args& a, hipStream_t s) {
   // blocks that hold a chunk's tokens: at most one more than the chunk fills, each side
   const int64_t blocks = a.T / kBlockSize + 2 * static_cast<int64_t>(a.B);
   const int64_t append = 1 + (blocks * a.Hkv + kApWaves - 1) / kApWaves;
-  const int64_t merge = a.ranges > 1 ? static_cast<int64_t>(a.max_tiles) * 4 * a.Hkv : 0;
+  const int64_t merge = a.ranges > 1 ? static_cast<int64_t>(a.max_tiles) * (kP4Rows / merge_rows<D>()) * a.Hkv : 0;
   if (units >= (1LL << 31) || append >= (1LL << 31) || merge >= (1LL << 31))
     return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: %lld units, grids of %lld and %lld workgroups",
                       who, (long long)units, (long long)append, (long long)merge);
