@@ -391,9 +391,16 @@ void launch_kv4(const DecodeArgs& a, int B, unsigned grid, int W, hipStream_t s)
     decode_kv4_kernel<D, kKv4Depth, RANKED, 1, WEIGHTED><<<grid, kWave, 0, s>>>(a, B);
 }
 
+// Waves that share a partition, by units as for bf16, but later: a block takes a quarter
+// of the time, so what a wave does before its first block weighs more. Measured in us
+// with 1 / 2 / 4 waves, 8 KV heads of 4 query heads: 1024 units 27 / 21 / 19 (16 requests
+// of up to 4000 tokens), 1200 28 / 22.5 / 21.6, 2112 34 / 31 / 33, 4224 37.8 / 36.7 / 38.6;
+// one query head per KV head: 1024 20 / 15.8 / 15.2, 8192 61 / 64 / 71. Requests of one
+// partition fill it in part only: 1024 units 16.4 / 15.2 / 18.8.
 int kv4_waves(const DecodeArgs& a, int B) {
   const int64_t units = static_cast<int64_t>(a.Hkv) * B * a.n_parts;
-  return units < 512 ? 4 : units < 2048 ? 2 : 1;
+  if (units < (a.n_parts > 1 ? 1536 : 512)) return 4;
+  return units < (a.n_parts > 1 ? 5120 : 2048) ? 2 : 1;
 }
 
 template <int D>
@@ -405,7 +412,10 @@ local_status_t launch_decode_kv4(const DecodeArgs& a, int B, hipStream_t s) {
                       (long long)std::max(wgs, merge));
   const unsigned grid = static_cast<unsigned>(wgs);
   const int W = kv4_waves(a, B);
-  if (B <= kRankChunks * kWave)
+  // (units that are all resident at once need no order, and finding it takes a call of
+  // 4 requests 1 us of 6.7)
+  const bool ranked = B <= kRankChunks * kWave && wgs * W > 2048;
+  if (ranked)
     a.w_out ? launch_kv4<D, true, true>(a, B, grid, W, s)
             : launch_kv4<D, true, false>(a, B, grid, W, s);
   else
