@@ -15,6 +15,11 @@ the whole step can also be captured into a HIP graph by the caller. The q, k
 and v projections read the same x, so those with the same adapter setup run
 as one grouped call (local_lora_linear_grouped): one pass of launches over
 their concatenated weights.
+
+A uint8 pool is a 4-bit pool: the step then attends over it
+(local_paged_attn_decode_kv4/_prefill_kv4). With `block_weight` a decode step
+adds up, over its layers, how much attention weight each block of a request
+receives (what local_kv_evict cuts contexts down by).
 """
 from __future__ import annotations
 
@@ -58,25 +63,35 @@ class Step:
 
     weights[l] maps "W_q", "A_q", "B_q", "ranks_q", ... to device tensors
     (adapter entries only for projections that carry adapters).
-    kv_pool is [n_layers, 2, num_blocks, Hkv, 16*D] bf16.
+    kv_pool is [n_layers, 2, num_blocks, Hkv, 16*D] bf16, or a 4-bit pool
+    [n_layers, num_blocks, Hkv, 17*D] uint8.
+    block_weight (decode only) is [B, max_blocks] float32, updated in place: each
+    step multiplies it by weight_decay and adds the weights of all layers.
     """
 
     def __init__(self, kind: str, x: torch.Tensor, weights: List[Dict[str, torch.Tensor]],
                  meta: StepMeta, kv_pool: torch.Tensor, hq: int, hkv: int, head_dim: int,
-                 residual: bool, stale_cap: Optional[int] = None):
+                 residual: bool, stale_cap: Optional[int] = None,
+                 block_weight: Optional[torch.Tensor] = None, weight_decay: float = 1.0):
         assert kind in ("decode", "prefill")
+        if block_weight is not None and kind != "decode":
+            raise ValueError("block_weight belongs to decode steps")
+        four_bit = kv_pool.dtype == torch.uint8
+        # the version check rides on the first layer's attention where that is the plain
+        # bf16 decode
+        folded = kind == "decode" and not four_bit and block_weight is None
         dev = x.device
         T, H = x.shape
         D = head_dim
         self.kind = kind
         self.n_layers = len(weights)
-        self.inputs = (x, weights, meta, kv_pool)  # owned for the step's lifetime
+        self.inputs = (x, weights, meta, kv_pool, block_weight)  # owned for the step's lifetime
         self.ws = bd.Workspace(dev)
         self.calls: List[bd.Call] = []
         self.buffers = {}
         cap = stale_cap if stale_cap is not None else meta.block_table.numel()
-        self.version_check = None  # a separate call only in prefill
-        if kind == "prefill":
+        self.version_check = None  # a separate call where it is not folded
+        if not folded:
             self.version_check = bd.prepare_block_version_check(
                 meta.block_table, meta.ctx_lens, meta.block_version, meta.req_version, cap=cap,
                 workspace=self.ws)
@@ -99,8 +114,24 @@ class Step:
             y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
             lse = torch.empty((T, hq), dtype=torch.float32, device=dev)
             lc = {"in": self._in_proj(lw, xin, {"q": q, "k": k, "v": v}, meta)}
-            kc, vc = kv_pool[l, 0], kv_pool[l, 1]
-            if kind == "decode" and l == 0:
+            tags = (meta.block_table, meta.ctx_lens, meta.block_version, meta.req_version)
+            new = dict(k_new=k.view(T, hkv, D), v_new=v.view(T, hkv, D), out=o.view(T, hq, D),
+                       lse=lse, workspace=self.ws)
+            if block_weight is not None:
+                new.update(weight_in=block_weight, weight_out=block_weight,
+                           weight_decay=weight_decay if l == 0 else 1.0)
+            if not four_bit:
+                kc, vc = kv_pool[l, 0], kv_pool[l, 1]
+            if four_bit and kind == "decode":
+                lc["attn"] = bd.prepare_paged_attn_decode_kv4(
+                    q.view(T, hq, D), kv_pool[l], *tags, sm_scale, **new)
+            elif four_bit:
+                lc["attn"] = bd.prepare_paged_attn_prefill_kv4(
+                    q.view(T, hq, D), meta.q_indptr, kv_pool[l], *tags, sm_scale, **new)
+            elif block_weight is not None:
+                lc["attn"] = bd.prepare_paged_attn_decode_weighted(
+                    q.view(T, hq, D), kc, vc, *tags, sm_scale, Hkv=hkv, **new)
+            elif kind == "decode" and l == 0:
                 pairs, n_stale, valid = self.version_outputs
                 lc["attn"] = bd.prepare_paged_attn_decode_checked(
                     q.view(T, hq, D), kc, vc, meta.block_table, meta.ctx_lens,

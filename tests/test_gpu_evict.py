@@ -1,6 +1,4 @@
-"""Block weights of bf16 decode, eviction, and a run of everything together.
-
-Tolerances as in test_gpu_kv4.py.
+"""Block weights of bf16 decode, eviction, and a run of everything together (tolerances: kv4_helpers.py).
 """
 from __future__ import annotations
 
@@ -11,10 +9,10 @@ import pytest
 import torch
 
 import paper_2608_15241_amd as lk
-from gpu_helpers import dev, dev_u16, f64, say
 from oracle import kv4
-from pool_helpers import bits_to_f64, dense_to_pool, f32_to_bf16_bits, make_table
-from test_gpu_kv4 import check_out, check_weight
+from tests.gpu_helpers import dev, dev_u16, f64, say
+from tests.kv4_helpers import check_out, check_weight
+from tests.pool_helpers import bits_to_f64, dense_to_pool, f32_to_bf16_bits, make_table
 
 pytestmark = pytest.mark.gpu
 BS = 16
@@ -241,3 +239,99 @@ def test_a_context_that_is_rounded_decoded_evicted_and_continued(D, hq, hkv):
     ref, ref_lse, size, _ = kv4.attention(bits_to_f64(q), starts, ctx, table, tags, version,
                                           *kv4.unpack(tiles), sm)
     check_out(out, lse, ref, ref_lse, size, "prefill")
+
+
+@pytest.mark.parametrize("four_bit", [True, False])
+def test_step_with_weights(four_bit):
+    """Two chained decode layers through Step, over a 4-bit pool and a bf16 one: each
+    layer's attention against the definition on the step's own q, k and v, the weights of
+    both layers in one array, the version check beside, replayed from a graph."""
+    from paper_2608_15241_amd.step import Step, StepMeta
+    rng = np.random.default_rng(9)
+    B, hq, hkv, D, H, layers = 3, 4, 2, 64, 256, 2
+    ctx = np.array([70, 33, 200], np.int32)
+    table, num = make_table(rng, ctx, extra_blocks=1, max_blocks=16)
+    tags, version = np.full(num, 8, np.int32), np.full(B, 8, np.int32)
+    tags[table[2, 4]] = 7
+    kd, vd = (f32_to_bf16_bits(rng.standard_normal((layers, num, hkv, BS, D))) for _ in range(2))
+    bf = lambda *s, std=1.0: dev_u16(f32_to_bf16_bits(rng.standard_normal(s) * std))  # noqa: E731
+    weights = [{"W_q": bf(hq * D, H, std=0.05), "W_k": bf(hkv * D, H, std=0.05),
+                "W_v": bf(hkv * D, H, std=0.05), "W_o": bf(H, hq * D, std=0.05)}
+               for _ in range(layers)]
+    pool = torch.stack([torch.stack([dev_u16(x).view(num, hkv, BS * D)
+                                     for x in dense_to_pool(kd[l], vd[l])])
+                        for l in range(layers)])
+    if four_bit:
+        pool = torch.stack([lk.local_kv4_pool_import(pool[l, 0], pool[l, 1])
+                            for l in range(layers)])
+    meta = StepMeta(block_table=dev(table), ctx_lens=dev(ctx), block_version=dev(tags),
+                    req_version=dev(version), q_indptr=dev(np.arange(B + 1)),
+                    token_adapter=dev(np.full(B, -1)),
+                    token_scale=torch.zeros(B, device="cuda"), T=B, B=B)
+    w = torch.ones((B, 16), device="cuda")
+    step = Step("decode", bf(B, H), weights, meta, pool, hq, hkv, D, residual=False,
+                block_weight=w, weight_decay=0.5)
+    step()
+    first = w.clone()
+    total = np.where(np.arange(16) < ((ctx + 15) // 16)[:, None], 0.5, 0.0)
+    at = (table[np.arange(B), (ctx - 1) // BS], (ctx - 1) % BS)
+    for l in range(layers):
+        buf = step.buffers[l]
+        kn, vn = (f64(buf[n]).reshape(B, hkv, D) for n in "kv")
+        if four_bit:
+            tiles = kv4.write(kv4.pack(bits_to_f64(kd[l]), bits_to_f64(vd[l])), kn, vn, *at)
+            assert np.array_equal(pool[l].cpu().numpy(), tiles)
+            k, v = kv4.unpack(tiles)
+        else:
+            k, v = bits_to_f64(kd[l]), bits_to_f64(vd[l])
+            k[at[0], :, at[1]], v[at[0], :, at[1]] = kn, vn
+        ref, ref_lse, size, more = kv4.attention(f64(buf["q"]).reshape(B, hq, D), np.arange(B + 1),
+                                                 ctx, table, tags, version, k, v,
+                                                 1.0 / math.sqrt(D))
+        check_out(buf["o"].view(B, hq, D), buf["lse"], ref, ref_lse, size, "layer %d" % l)
+        total = total + more
+    check_weight(first, total, "weights")
+    assert int(step.version_outputs[1]) == 1
+    assert step.version_outputs[0][0].tolist() == [2, 4]
+    out = step.out.clone()
+    g = step.capture()
+    for r in range(3):
+        w.fill_(1.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(step.out, out) and torch.equal(w, first)
+    with pytest.raises(ValueError):
+        Step("prefill", bf(B, H), weights, meta, pool, hq, hkv, D, residual=False, block_weight=w)
+
+
+def test_prefill_step_over_the_4_bit_pool():
+    """A chunked-prefill step whose projections feed the 4-bit append and attention."""
+    from paper_2608_15241_amd.step import Step, StepMeta
+    rng = np.random.default_rng(10)
+    chunk, prefix, hq, hkv, D, H = np.array([40, 7]), np.array([25, 90]), 8, 2, 128, 256
+    ctx = (chunk + prefix).astype(np.int32)
+    table, num = make_table(rng, ctx)
+    tags, version = np.full(num, 1, np.int32), np.ones(2, np.int32)
+    starts = np.concatenate([[0], np.cumsum(chunk)])
+    tiles = kv4.pack(*rng.standard_normal((2, num, hkv, BS, D)))
+    pool = torch.from_numpy(tiles[None].copy()).to("cuda")
+    bf = lambda *s, std=1.0: dev_u16(f32_to_bf16_bits(rng.standard_normal(s) * std))  # noqa: E731
+    weights = [{"W_q": bf(hq * D, H, std=0.05), "W_k": bf(hkv * D, H, std=0.05),
+                "W_v": bf(hkv * D, H, std=0.05), "W_o": bf(H, hq * D, std=0.05)}]
+    T = int(chunk.sum())
+    meta = StepMeta(block_table=dev(table), ctx_lens=dev(ctx), block_version=dev(tags),
+                    req_version=dev(version), q_indptr=dev(starts),
+                    token_adapter=dev(np.full(T, -1)), token_scale=torch.zeros(T, device="cuda"),
+                    T=T, B=2)
+    step = Step("prefill", bf(T, H), weights, meta, pool, hq, hkv, D, residual=False)
+    step()
+    buf = step.buffers[0]
+    row = np.repeat(np.arange(2), chunk)
+    pos = np.concatenate([np.arange(p, p + n) for p, n in zip(prefix, chunk)])
+    kv4.write(tiles, *(f64(buf[n]).reshape(T, hkv, D) for n in "kv"), table[row, pos // BS],
+              pos % BS)
+    assert np.array_equal(pool[0].cpu().numpy(), tiles)
+    ref, ref_lse, size, _ = kv4.attention(f64(buf["q"]).reshape(T, hq, D), starts, ctx, table, tags,
+                                          version, *kv4.unpack(tiles), 1.0 / math.sqrt(D))
+    check_out(buf["o"].view(T, hq, D), buf["lse"], ref, ref_lse, size, "out")
+    assert int(step.version_outputs[1]) == 0

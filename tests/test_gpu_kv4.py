@@ -1,14 +1,5 @@
 """The 4-bit pool on the GPU: conversion bit by bit, decode and prefill attention against
-float64.
-
-Tolerance of an attention output (per value): the weights are rounded to bf16 before the
-value product (half a step, 2^-8 of each weight), so the sum is off by at most 2^-8 of
-S = sum w |v|; the result is rounded once (2^-8 of it). A score is a float32 sum of D
-products of magnitude |q||k| sm: off by at most (D + 2) 2^-24 sum |q k| sm, below 5e-5
-for the inputs here, as is the exponential, so weights and lse are off by 2 * 5e-5
-relative, 1e-4 S in the output. With 1% on top of the two roundings for their product:
-    |out - ref| <= 1.01 * 2^-8 (S + |ref|) + 2e-4 S,    |lse - ref| <= 2e-4,
-and a block's weight, a sum of such weights, is off by at most 3e-4 of itself.
+float64 (tolerances: kv4_helpers.py).
 """
 from __future__ import annotations
 
@@ -19,30 +10,13 @@ import pytest
 import torch
 
 import paper_2608_15241_amd as lk
-from gpu_helpers import dev, dev_u16, f64, say
 from oracle import kv4
-from pool_helpers import bits_to_f64, dense_to_pool, f32_to_bf16_bits
+from tests.gpu_helpers import dev, dev_u16, f64, say
+from tests.kv4_helpers import check_out, check_weight
+from tests.pool_helpers import bits_to_f64, dense_to_pool, f32_to_bf16_bits
 
 pytestmark = pytest.mark.gpu
 BS = 16
-
-
-def check_out(out, lse, ref, ref_lse, size, name):
-    out, lse = f64(out), f64(lse)
-    nan = np.isnan(ref)
-    assert np.array_equal(np.isnan(out), nan), name
-    err = np.abs(out - ref)[~nan]
-    tol = (1.01 * 2.0 ** -8 * (size + np.abs(ref)) + 2e-4 * size)[~nan]
-    assert (err <= tol).all(), "%s: off by %.3g where %.3g is allowed" % (
-        name, (err - tol).max(), tol[(err - tol).argmax()])
-    assert np.array_equal(np.isneginf(lse), np.isneginf(ref_lse)), name
-    assert np.array_equal(np.isnan(lse), np.isnan(ref_lse)), name
-    fine = np.isfinite(ref_lse)
-    assert (np.abs(lse[fine] - ref_lse[fine]) <= 2e-4).all(), name
-
-
-def check_weight(got, ref, name):
-    assert (np.abs(got.cpu().numpy() - ref) <= 3e-4 * np.abs(ref) + 1e-12).all(), name
 
 
 class Case:
