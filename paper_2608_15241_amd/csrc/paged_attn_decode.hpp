@@ -277,6 +277,11 @@ __device__ void decode_version_check(const DecodeArgs& a, int b, int B, int* sh)
   }
 }
 
+// Where block j of request b, KV head g, records its heads' weights.
+__device__ __forceinline__ float* blk_lse_at(const DecodeArgs& a, int b, int g, int j) {
+  return a.blk_lse + ((static_cast<int64_t>(b) * a.Hkv + g) * a.max_blocks + j) * a.group;
+}
+
 // Attention weight of D blocks of one request: w_out = decay * w_in + the sum over
 // the query heads of exp2(blk_lse - lse), with each head's lse over all blocks
 // taken from the partitions' sums again (a few KB from L2) rather than from the
@@ -288,19 +293,42 @@ __device__ void decode_block_weights(const DecodeArgs& a, int unit, float* lse2)
   const int b = unit / chunks, j = unit % chunks * D + static_cast<int>(threadIdx.x);
   const int nb = owned_blocks(a.ctx_lens[b], a.max_blocks);
   const int np = max(1, full_parts(nb + a.pb - 1, a.pb));
+  // The block's own values first: they need no sum, and their loads run beside those of
+  // the partitions' sums.
+  constexpr int kAhead = 8;  // groups of 4 heads read ahead
+  const int64_t at = static_cast<int64_t>(b) * a.max_blocks + j;
+  const bool mine = j < nb, fours = a.group % 4 == 0;
+  auto values = [&](int q) {  // heads 4 q ..
+    const int per = a.group / 4;
+    return *reinterpret_cast<const f32x4*>(blk_lse_at(a, b, q / per, j) + q % per * 4);
+  };
+  f32x4 ahead[kAhead];
+  if (mine && fours) {
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q)
+      if (4 * q < a.Hq) ahead[q] = values(q);
+  }
+  const float old = mine && a.w_in ? a.w_in[at] : 0.f;
   if (unit % chunks * D < nb) {
-    constexpr int kPer = 4;  // lanes that share a head's partitions
+    constexpr int kPer = 4, kBatch = 4;  // lanes that share a head's partitions
     const int p0 = threadIdx.x % kPer;
     for (int h0 = 0; h0 < a.Hq; h0 += D / kPer) {
       const int h = min(h0 + static_cast<int>(threadIdx.x) / kPer, a.Hq - 1);
       const float2* ml = reinterpret_cast<const float2*>(
           a.part_ml + (static_cast<int64_t>(b) * a.Hq + h) * a.n_parts * 2);
       float M = kNegBig, den = 0.f;
-      for (int p = p0; p < np; p += kPer) {
-        const float2 v = ml[p];
-        const float Mn = fmaxf(M, v.x);
-        den = den * fast_exp2(M - Mn) + v.y * fast_exp2(v.x - Mn);
-        M = Mn;
+      for (int p = p0; p < np; p += kPer * kBatch) {
+        float2 v[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          v[i] = p + kPer * i < np ? ml[p + kPer * i] : float2{kNegBig, 0.f};
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) top = fmaxf(top, v[i].x);
+        den *= fast_exp2(M - top);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) den += v[i].y * fast_exp2(v[i].x - top);
+        M = top;
       }
       float top = fmaxf(M, __shfl_xor(M, 1));
       top = fmaxf(top, __shfl_xor(top, 2));
@@ -313,23 +341,23 @@ __device__ void decode_block_weights(const DecodeArgs& a, int unit, float* lse2)
   }
   __syncthreads();
   if (j >= a.max_blocks) return;
-  const int64_t at = static_cast<int64_t>(b) * a.max_blocks + j;
   float w = 0.f;
-  if (j < nb) {
-    for (int g = 0; g < a.Hkv; ++g) {
-      const float* bl =
-          a.blk_lse + ((static_cast<int64_t>(b) * a.Hkv + g) * a.max_blocks + j) * a.group;
-      const float* l = lse2 + g * a.group;
-      int e = 0;
-      if (a.group % 4 == 0)
-        for (; e < a.group; e += 4) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(bl + e);
+  if (mine) {
+    if (fours) {
+      for (int q0 = 0; 4 * q0 < a.Hq; q0 += kAhead) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w += fast_exp2(v[i] - l[e + i]);
+        for (int q = 0; q < kAhead; ++q) {
+          if (4 * (q0 + q) >= a.Hq) break;
+          const f32x4 v = q0 == 0 ? ahead[q] : values(q0 + q);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w += fast_exp2(v[i] - lse2[4 * (q0 + q) + i]);
         }
-      for (; e < a.group; ++e) w += fast_exp2(bl[e] - l[e]);
+      }
+    } else {
+      for (int h = 0; h < a.Hq; ++h)
+        w += fast_exp2(blk_lse_at(a, b, h / a.group, j)[h % a.group] - lse2[h]);
     }
-    if (a.w_in) w = fmaf(a.w_decay, a.w_in[at], w);
+    if (a.w_in) w = fmaf(a.w_decay, old, w);
   }
   a.w_out[at] = w;
 }
@@ -365,9 +393,10 @@ __global__ __launch_bounds__(D) void decode_merge_kernel(DecodeArgs a, int B) {
   const int nb = owned_blocks(L, a.max_blocks);
   const int np = max(1, full_parts(nb + a.pb - 1, a.pb));
   if (np == 1) return;  // written by the main kernel
-  // one pass over the partitions, 8 at a time with all their loads in flight;
-  // the running sums are rescaled when a batch raises the maximum
-  constexpr int kMergeBatch = 8;
+  // one pass over the partitions, 8 at a time (16 of the 4-bit pool's, whose calls are
+  // shorter) with all their loads in flight; the running sums are rescaled when a batch
+  // raises the maximum
+  constexpr int kMergeBatch = NANS ? 16 : 8;
   const float* ml = a.part_ml + static_cast<int64_t>(bh) * a.n_parts * 2;
   const float* po = a.part_o + static_cast<int64_t>(bh) * a.n_parts * D;
   float M = kNegBig, den = 0.f, num = 0.f;
@@ -433,10 +462,6 @@ __device__ __forceinline__ float sum_kgroups2(float a, float b) {
   return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
-// Where block j of request b, KV head g, records its heads' weights.
-__device__ __forceinline__ float* blk_lse_at(const DecodeArgs& a, int b, int g, int j) {
-  return a.blk_lse + ((static_cast<int64_t>(b) * a.Hkv + g) * a.max_blocks + j) * a.group;
-}
 
 // Split-KV partials of a call: the partition length (a->pb, a->n_parts) and what
 // the partials take.

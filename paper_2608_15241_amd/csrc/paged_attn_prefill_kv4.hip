@@ -275,7 +275,6 @@ __global__ __launch_bounds__(kApThreads) void append_kv4_kernel(Prefill4Args a) 
   int b, j;
   if (!find_new_block(a, unit / a.Hkv, &b, &j)) return;
   const int p = a.block_table[static_cast<int64_t>(b) * a.max_blocks + j];
-  if (p < 0 || p >= a.num_blocks) return;
   const int r0 = a.q_indptr[b], n = a.q_indptr[b + 1] - r0;
   const int first = a.ctx_lens[b] - n;  // position of the chunk's first token
   // Slot s of the block is token row s + off of the chunk where that is one of its n.
@@ -284,7 +283,6 @@ __global__ __launch_bounds__(kApThreads) void append_kv4_kernel(Prefill4Args a) 
   auto row = [&](int slot) {
     return (static_cast<int64_t>(r0 + slot + off) * a.Hkv + g) * D;
   };
-  uint8_t* o = a.kv4 + (static_cast<int64_t>(p) * a.Hkv + g) * L4::kTile;
   // A lane takes the same dims of K and V, VT col .., of slots 4 kgrp .. (whole rows are
   // read side by side; K by the lane that holds its codes in attention read 64 places).
   auto read = [&](const uint16_t* x, int e) {
@@ -303,6 +301,8 @@ __global__ __launch_bounds__(kApThreads) void append_kv4_kernel(Prefill4Args a) 
   u32x4 kv[4], vv[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) kv[e] = read(a.k_new, e), vv[e] = read(a.v_new, e);
+  if (p < 0 || p >= a.num_blocks) return;  // (read while the id was on its way)
+  uint8_t* o = a.kv4 + (static_cast<int64_t>(p) * a.Hkv + g) * L4::kTile;
   uint32_t kcode[4], ks[4], vcode[4], vs[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
