@@ -15,6 +15,8 @@
 //  * Blocks are taken in pairs: the value product then is a 16x16x32 (32 keys), and
 //    the running maximum, the rescale and the cross-lane steps come once a pair.
 //  * Partitions, dispatch order, waves per partition and merge: as for bf16.
+#include <type_traits>
+
 #include "kv4.hpp"
 #include "paged_attn_decode.hpp"
 
@@ -258,13 +260,35 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
       const float sum = sum_kgroups2(ps[0], ps[1]);
       if (kgrp < 2 && col < G && i >= 0) bl[i * G] = m_run + __log2f(sum);
     }
-    u32x2 va[VT], vb[VT];
-    unpack_v<D>(R.v[0], R.vs[0], va);
-    unpack_v<D>(R.v[1], R.vs[1], vb);
+    float vs[2][4];
 #pragma unroll
-    for (int t = 0; t < VT; ++t)
-      acc[t] = mfma16x16x32(as_bf16x8(u32x4{va[t].x, va[t].y, vb[t].x, vb[t].y}), as_bf16x8(pf),
-                            acc[t]);
+    for (int e = 0; e < 2; ++e) {
+      vs[e][0] = scale4_of<0>(R.vs[e]);
+      vs[e][1] = scale4_of<1>(R.vs[e]);
+      vs[e][2] = scale4_of<2>(R.vs[e]);
+      vs[e][3] = scale4_of<3>(R.vs[e]);
+    }
+    auto pair_tiles = [&](auto byte) {  // tiles 2 i and 2 i + 1: byte i of a token's codes
+      constexpr int I = decltype(byte)::value;
+      u32x4 lo, hi;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t x0 = unpack4<I>(v_token<D>(R.v[e], 2 * k), vs[e][2 * k]);
+          const uint32_t x1 = unpack4<I>(v_token<D>(R.v[e], 2 * k + 1), vs[e][2 * k + 1]);
+          lo[2 * e + k] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+          hi[2 * e + k] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+        }
+      acc[2 * I] = mfma16x16x32(as_bf16x8(lo), as_bf16x8(pf), acc[2 * I]);
+      acc[2 * I + 1] = mfma16x16x32(as_bf16x8(hi), as_bf16x8(pf), acc[2 * I + 1]);
+    };
+    pair_tiles(std::integral_constant<int, 0>());
+    pair_tiles(std::integral_constant<int, 1>());
+    if constexpr (D == 128) {
+      pair_tiles(std::integral_constant<int, 2>());
+      pair_tiles(std::integral_constant<int, 3>());
+    }
   };
 
   // ring of DEPTH pairs: DEPTH-1 pairs load while one computes

@@ -163,6 +163,8 @@ DECODE = [
     ([1025, 2000, 512, 513], 8, 8, 64, dict(stale=0.05)),
     ([300] * 9, 32, 4, 128, dict(stale=0.5)),
     ([40], 3, 3, 128, dict(width=2)),  # longer than its table
+    ([9000, 300], 8, 1, 64, dict(width=600, stale=0.05)),
+    ([60, 20], 40, 10, 64, {}),
 ]
 
 
@@ -187,6 +189,23 @@ def test_decode(i, append, weighted):
         out, lse = lk.local_paged_attn_decode_kv4(q, pool, *meta, c.sm, **new)
     check_out(out, lse, ref, ref_lse, size, "out")
     assert np.array_equal(pool.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("sm", [-0.3, 0.0, 1e-30, 4.0])
+def test_softmax_scales(sm):
+    """Negative, zero (every visible key weighs the same), vanishing and large scales."""
+    c = Case(77, [100, 37], 8, 2, 128, new=[20, 37], stale=0.2)
+    c.sm = sm
+    q, pool, meta, new = c.gpu()
+    ref, ref_lse, size, _ = c.ref(c.appended())
+    out, lse = lk.local_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, sm, **new)
+    # (scores are up to 4 / 0.088 times those of the other tests, and so are their errors)
+    wide = max(1.0, abs(sm) * math.sqrt(128))
+    check_out(out, lse, ref, ref_lse, size, "prefill", wide)
+    last = c.starts[1:] - 1
+    out, lse = lk.local_paged_attn_decode_kv4(q[torch.from_numpy(last.astype(np.int64))].contiguous(),
+                                              pool, *meta, sm)
+    check_out(out, lse, ref[last], ref_lse[last], size[last], "decode", wide)
 
 
 def test_decode_of_many_requests():
@@ -237,6 +256,7 @@ PREFILL = [
     ([1700, 5], [2, 33], 4, 1, 128, dict(stale=0.1, width=130)),
     ([4500], [20], 2, 2, 64, {}),
     ([0], [300], 2, 1, 128, {}),
+    ([20], [30], 4, 2, 64, dict(width=2)),  # longer than its table
 ]
 
 
