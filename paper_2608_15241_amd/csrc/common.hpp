@@ -134,6 +134,27 @@ __device__ __forceinline__ float max_xor32(float v) {
   return max2f(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Sum of v over the k-groups (lanes l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float sum_kgroups(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+// The same of two values at once: k-groups 0 and 2 return the sum of a, 1 and 3 of b.
+__device__ __forceinline__ float sum_kgroups2(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false,
+                                                  false);
+  const float v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+
 // ---------------------------------------------------------------- math
 __device__ __forceinline__ float fast_exp2(float x) {
   return __builtin_amdgcn_exp2f(x);

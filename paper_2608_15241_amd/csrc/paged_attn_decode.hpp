@@ -442,27 +442,6 @@ inline size_t block_lse_bytes(int B, int Hq, int max_blocks) {
   return align256(static_cast<size_t>(B > 0 ? B : 1) * Hq * max_blocks * sizeof(float));
 }
 
-// Sum of v over the k-groups (lanes l, l ^ 16, l ^ 32, l ^ 48).
-__device__ __forceinline__ float sum_kgroups(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
-                                                  false);
-  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
-                                                  false);
-  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
-}
-
-// The same of two values at once: k-groups 0 and 2 return the sum of a, 1 and 3 of b.
-__device__ __forceinline__ float sum_kgroups2(float a, float b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false,
-                                                  false);
-  const float v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
-                                                  false);
-  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
-}
-
-
 // Split-KV partials of a call: the partition length (a->pb, a->n_parts) and what
 // the partials take.
 struct DecodeParts {

@@ -12,36 +12,13 @@
 //    order (kv4.hpp), a conversion makes two scaled values, and V needs one lane-local
 //    permute per two values to pair neighbouring tokens: 1.3 instructions a value and
 //    lane group, of which the scales are 0.2.
-//  * Blocks are taken in pairs: the value product then is a 16x16x32 (32 keys), and
-//    the running maximum, the rescale and the cross-lane steps come once a pair.
+//  * Blocks are taken in pairs (kv4_attn.hpp).
 //  * Partitions, dispatch order, waves per partition and merge: as for bf16.
-#include <type_traits>
-
-#include "kv4.hpp"
+#include "kv4_attn.hpp"
 #include "paged_attn_decode.hpp"
 
 namespace localk {
 namespace {
-
-// One pair of blocks in registers, as loaded.
-template <int D>
-struct Regs4 {
-  uint32_t k[2][D / 32];  // this lane's codes of K and V
-  uint32_t v[2][D / 32];
-  uint32_t ks[2], vs[2];  // the scale of its K dims; the scales of its 4 tokens of V
-};
-
-template <int D>
-__device__ __forceinline__ void load_codes(__amdgpu_buffer_rsrc_t r, uint32_t off,
-                                           uint32_t (&c)[D / 32]) {
-  if constexpr (D == 128) {
-    const u32x4 v = buf_load16_stream(r, off);
-    c[0] = v.x, c[1] = v.y, c[2] = v.z, c[3] = v.w;
-  } else {
-    const u32x2 v = buf_load8_stream(r, off);
-    c[0] = v.x, c[1] = v.y;
-  }
-}
 
 // The new token as a lane holds it: its K dims (D/4, one scale) where the lane's
 // column is the token's slot, its V dims (D/16) where its k-group holds the slot.
@@ -66,15 +43,12 @@ __device__ __forceinline__ void quantise_new(const uint16_t* k_new, const uint16
   n.vs = round_v<D>(vv, n.v);
 }
 
-constexpr float kLazy4 = 8.f;  // log2 of the largest weight before the maximum rises
-
 // __launch_bounds__: three waves a SIMD (registers permitting, and they do: two ran the
 // 128 contexts of 1K to 16K tokens 3% slower).
 template <int D, int DEPTH, bool RANKED, int W, bool WEIGHTED>
 __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, int B) {
   using L4 = Kv4<D>;
   constexpr int KC = D / 32;
-  constexpr int VT = D / 16;
 
   const int lane = threadIdx.x % kWave;
   const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -127,20 +101,12 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
     }
   }
 
-  // Query heads of this KV head as the B operand (column = head); a lane's dims are
-  // those of its codes of K.
-  bf16x8 qv[KC];
-  {
-    const int h = g * G + col;
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      u32x4 v = {0u, 0u, 0u, 0u};
-      if (col < G)
-        v = ld_global<u32x4>(a.q + (static_cast<int64_t>(b) * a.Hq + h) * D + (D / 4) * kgrp +
-                             8 * c);
-      qv[c] = as_bf16x8((v ^ a.q_xor) & a.q_and);
-    }
-  }
+  // Rows: the query heads of this KV head.
+  const int64_t bh0 = static_cast<int64_t>(b) * a.Hq + g * G;
+  Attn4<D> at;
+  at.load_q(a.q + (bh0 + col) * D, col < G, a.q_xor, a.q_and);
+  const float inv_scale = 1.f / a.scale_log2;
+  at.init(inv_scale);
 
   // The new token (position L-1), if its block is in this partition: substituted while
   // the block is read, written after the last block.
@@ -157,12 +123,6 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
     quantise_new<D>(a.k_new + row, a.v_new + row, col, kgrp, fresh);
   }
 
-  f32x4 acc[VT];
-#pragma unroll
-  for (int t = 0; t < VT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = kNegBig, l_run = 0.f;
-  const float inv_scale = 1.f / a.scale_log2;
-  float rise = (kNegBig + kLazy4) * inv_scale;  // a raw score above it raises m_run
   // (WEIGHTED) where this lane records block j0's weight
   float* bl = blk_lse_at(a, b, g, j0) + col;
 
@@ -173,16 +133,8 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
     return i;
   };
   auto load_block = [&](Regs4<D>& R, int e, int i) {
-    const bool live = i >= 0;
-    const int p = live ? __builtin_amdgcn_readlane(my_phys, i) : 0;
-    const int64_t tile = (static_cast<int64_t>(p) * a.Hkv + g) * L4::kTile;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.kv4 + tile, live ? L4::kTile : 0u);
-    load_codes<D>(r, lane * L4::kLane, R.k[e]);
-    load_codes<D>(r, L4::kV + lane * L4::kLane, R.v[e]);
-    R.ks[e] = __builtin_amdgcn_raw_buffer_load_b8(r, L4::k_scale(L4::k_group(kgrp), col), 0,
-                                                  0);
-    R.vs[e] = __builtin_amdgcn_raw_buffer_load_b32(r, L4::v_scale(L4::v_group(col), 4 * kgrp), 0,
-                                                   0);
+    const int p = i >= 0 ? __builtin_amdgcn_readlane(my_phys, i) : 0;
+    load_block4<D>(R, e, a.kv4, static_cast<int64_t>(p) * a.Hkv + g, i >= 0);
   };
   // The block that holds the last position: the new token's codes for its slot; slots
   // past it as zeros (their contents are undefined and must not reach the product).
@@ -214,81 +166,23 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
       const int i = e ? i1 : i0;
       const bool tail = i < 0 || j0 + i == j_new;
       if (tail && i >= 0) fix_last(R, e);
-      const float ks = scale4(R.ks[e]);
-      sc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        const uint32_t w = R.k[e][c];
-        const u32x4 kf = {unpack4<0>(w, ks), unpack4<1>(w, ks), unpack4<2>(w, ks),
-                          unpack4<3>(w, ks)};
-        sc[e] = mfma16x16x32(as_bf16x8(kf), qv[c], sc[e]);
-      }
+      sc[e] = at.scores(R, e);
       if (tail) {  // no block, or one with slots past the context's end
         const int live = i < 0 ? 0 : L - (j0 + i) * kBlockSize;
 #pragma unroll
         for (int k = 0; k < 4; ++k) sc[e][k] = 4 * kgrp + k < live ? sc[e][k] : -INFINITY;
       }
     }
-    // The running maximum rises only when a weight would pass 2^kLazy4: below, the
-    // weights are exact all the same, and nothing has to cross lanes or be rescaled.
-    const float mx = max3f(max3f(sc[0][0], sc[0][1], sc[0][2]),
-                           max3f(sc[0][3], sc[1][0], sc[1][1]), max2f(sc[1][2], sc[1][3]));
-    if (__ballot(mx > rise)) {
-      const float m_new = fmaxf(m_run, max_xor32(max_xor16(mx)) * a.scale_log2);
-      const float alpha = fast_exp2(m_run - m_new);
-      l_run *= alpha;
-      m_run = m_new;
-      rise = (m_new + kLazy4) * inv_scale;
-#pragma unroll
-      for (int t = 0; t < VT; ++t) acc[t] *= alpha;
-    }
     float ps[2];
     u32x4 pf;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float p[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) p[k] = fast_exp2(fmaf(sc[e][k], a.scale_log2, -m_run));
-      ps[e] = (p[0] + p[1]) + (p[2] + p[3]);
-      pf[2 * e] = pack_bf16x2(p[0], p[1]);
-      pf[2 * e + 1] = pack_bf16x2(p[2], p[3]);
-    }
-    l_run += ps[0] + ps[1];
+    at.weigh(sc, a.scale_log2, inv_scale, ps, pf);
     if constexpr (WEIGHTED) {
       // k-group 0 ends up with the first block's sum, k-group 1 with the second's
       const int i = kgrp == 0 ? i0 : i1;
       const float sum = sum_kgroups2(ps[0], ps[1]);
-      if (kgrp < 2 && col < G && i >= 0) bl[i * G] = m_run + __log2f(sum);
+      if (kgrp < 2 && col < G && i >= 0) bl[i * G] = at.m_run + __log2f(sum);
     }
-    float vs[2][4];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      vs[e][0] = scale4_of<0>(R.vs[e]);
-      vs[e][1] = scale4_of<1>(R.vs[e]);
-      vs[e][2] = scale4_of<2>(R.vs[e]);
-      vs[e][3] = scale4_of<3>(R.vs[e]);
-    }
-    auto pair_tiles = [&](auto byte) {  // tiles 2 i and 2 i + 1: byte i of a token's codes
-      constexpr int I = decltype(byte)::value;
-      u32x4 lo, hi;
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t x0 = unpack4<I>(v_token<D>(R.v[e], 2 * k), vs[e][2 * k]);
-          const uint32_t x1 = unpack4<I>(v_token<D>(R.v[e], 2 * k + 1), vs[e][2 * k + 1]);
-          lo[2 * e + k] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
-          hi[2 * e + k] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
-        }
-      acc[2 * I] = mfma16x16x32(as_bf16x8(lo), as_bf16x8(pf), acc[2 * I]);
-      acc[2 * I + 1] = mfma16x16x32(as_bf16x8(hi), as_bf16x8(pf), acc[2 * I + 1]);
-    };
-    pair_tiles(std::integral_constant<int, 0>());
-    pair_tiles(std::integral_constant<int, 1>());
-    if constexpr (D == 128) {
-      pair_tiles(std::integral_constant<int, 2>());
-      pair_tiles(std::integral_constant<int, 3>());
-    }
+    at.values(R, pf);
   };
 
   // ring of DEPTH pairs: DEPTH-1 pairs load while one computes
@@ -336,11 +230,8 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
     }
   }
 
-  // ---- finish: the column's sum over the k-groups, then write. Accumulator t, row
-  // 4 kgrp + i is dim (4 kgrp + i) * VT + t, so a lane's dims are 4 * VT neighbours.
-  l_run = sum_kgroups(l_run);
-  const int64_t bh0 = static_cast<int64_t>(b) * a.Hq + g * G;
-  auto put = [&](int hc, int d, f32x4 num, float M, float den) {
+  extern __shared__ __attribute__((aligned(16))) float mg[];
+  at.template finish<W>(G, mg, [&](int hc, int d, f32x4 num, float M, float den) {
     const int64_t bh = bh0 + hc;
     if (n_parts_b == 1) {
       num *= den == 0.f ? 0.f : 1.f / den;
@@ -351,62 +242,18 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
       *reinterpret_cast<f32x4*>(a.part_o + (bh * a.n_parts + part) * D + d) = num;
     }
     if (d == 0 && (WEIGHTED || n_parts_b > 1)) {
-      const int64_t at = (bh * a.n_parts + part) * 2;
-      a.part_ml[at] = M;
-      a.part_ml[at + 1] = den;
+      const int64_t to = (bh * a.n_parts + part) * 2;
+      a.part_ml[to] = M;
+      a.part_ml[to + 1] = den;
     }
-  };
-  auto lane_dims = [&](int i, int t4) {  // accumulators 4 t4 .. + 3 of row 4 kgrp + i
-    return f32x4{acc[4 * t4][i], acc[4 * t4 + 1][i], acc[4 * t4 + 2][i], acc[4 * t4 + 3][i]};
-  };
-  if constexpr (W > 1) {
-    extern __shared__ __attribute__((aligned(16))) float mg[];
-    constexpr int kRow = D + 4;
-    float* mg_ml = mg + W * G * kRow;
-    if (col < G) {
-      const int row = wave * G + col;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t4 = 0; t4 < VT / 4; ++t4)
-          *reinterpret_cast<f32x4*>(mg + row * kRow + (4 * kgrp + i) * VT + 4 * t4) =
-              lane_dims(i, t4);
-      if (kgrp == 0) {
-        mg_ml[2 * row] = m_run;
-        mg_ml[2 * row + 1] = l_run;
-      }
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < G * (D / 4); e += kWave * W) {
-      const int hc = e / (D / 4), d = 4 * (e % (D / 4));
-      float M = kNegBig;
-#pragma unroll
-      for (int w = 0; w < W; ++w) M = fmaxf(M, mg_ml[2 * (w * G + hc)]);
-      float den = 0.f;
-      f32x4 num = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < W; ++w) {  // a wave without a block: weight x 0
-        const int row = w * G + hc;
-        const float f = fast_exp2(mg_ml[2 * row] - M);
-        den += mg_ml[2 * row + 1] * f;
-        num += *reinterpret_cast<const f32x4*>(mg + row * kRow + d) * f;
-      }
-      put(hc, d, num, M, den);
-    }
-  } else if (col < G) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int t4 = 0; t4 < VT / 4; ++t4)
-        put(col, (4 * kgrp + i) * VT + 4 * t4, lane_dims(i, t4), m_run, l_run);
-  }
+  });
 }
 
 constexpr int kKv4Depth = 2;  // pairs of blocks in registers
 
 template <int D, bool RANKED, bool WEIGHTED>
 void launch_kv4(const DecodeArgs& a, int B, unsigned grid, int W, hipStream_t s) {
-  const int lds = merge_lds_bytes<D>(W, a.group);
+  const int lds = join4_bytes<D>(W, a.group);
   if (W == 4)
     decode_kv4_kernel<D, kKv4Depth, RANKED, 4, WEIGHTED><<<grid, 4 * kWave, lds, s>>>(a, B);
   else if (W == 2)

@@ -28,7 +28,8 @@
 #include <algorithm>
 #include <climits>
 
-#include "kv4.hpp"
+#include "kv4_attn.hpp"
+#include "paged_attn_decode.hpp"
 
 namespace localk {
 namespace {
@@ -68,7 +69,8 @@ struct Prefill4Args {
   int64_t T, num_blocks;
   int B, Hq, Hkv, group, max_blocks;
   int ranges;      // the most a tile may be split into
-  int max_tiles;   // tiles that the plan has room for
+  int max_tiles;   // tiles that the plan has room for (of few rows: that there may be)
+  int pb;          // few rows: blocks of a partition, else 0
   float scale_log2;
   uint32_t q_xor, q_and;
 };
@@ -264,12 +266,12 @@ template <int D>
 __global__ __launch_bounds__(kApThreads) void append_kv4_kernel(Prefill4Args a) {
   using L4 = Kv4<D>;
   constexpr int VT = D / 16;
-  if (blockIdx.x == 0) {
+  if (a.plan && blockIdx.x == 0) {
     plan_kv4(a);
     return;
   }
-  const int64_t unit =
-      (static_cast<int64_t>(blockIdx.x) - 1) * kApWaves + threadIdx.x / kWave;
+  const int64_t unit = (static_cast<int64_t>(blockIdx.x) - (a.plan ? 1 : 0)) * kApWaves +
+                       threadIdx.x / kWave;
   const int lane = threadIdx.x % kWave, col = lane % 16, kgrp = lane / 16;
   const int g = static_cast<int>(unit % a.Hkv);
   int b, j;
@@ -829,23 +831,17 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   }
 }
 
-// Joins the key ranges of the tiles that have more than one: a thread takes 4 dims of a
-// row, a workgroup the rows that its threads make.
-template <int D>
-constexpr int merge_rows() { return kApThreads / (D / 4); }
+__device__ __forceinline__ void write_row(const Prefill4Args& a, int64_t q, int d, int D,
+                                          f32x4 num, float M, float den) {
+  num *= den == 0.f ? 0.f : 1.f / den;
+  *reinterpret_cast<u32x2*>(a.out + q * D + d) =
+      u32x2{pack_bf16x2(num[0], num[1]), pack_bf16x2(num[2], num[3])};
+  if (d == 0 && a.lse) a.lse[q] = den == 0.f ? -INFINITY : (M + __log2f(den)) * kLn2;
+}
 
+// Joins the n parts (key ranges) of dims d .. d + 3 of row q (token * Hq + query head).
 template <int D>
-__global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
-  const int g = blockIdx.x % a.Hkv;
-  const int rest = blockIdx.x / a.Hkv;
-  constexpr int kParts = kP4Rows / merge_rows<D>();
-  const int4 e = a.tiles[rest / kParts];
-  const int r0 = e.x, row0 = e.y, rows = e.z, n = e.w;
-  const int row = rest % kParts * merge_rows<D>() + threadIdx.x / (D / 4);
-  const int d = 4 * (threadIdx.x % (D / 4));
-  if (n == 1 || row >= rows) return;
-  const int at = row0 + row;
-  const int64_t q = static_cast<int64_t>(r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
+__device__ __forceinline__ void merge_row(const Prefill4Args& a, int64_t q, int d, int n) {
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml + q * a.ranges * 2);
   const float* po = a.part_o + q * a.ranges * D + d;
   // every range's loads in flight at once, 8 at a time
@@ -876,36 +872,283 @@ __global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
     }
     M = top;
   }
-  num *= den == 0.f ? 0.f : 1.f / den;
-  *reinterpret_cast<u32x2*>(a.out + q * D + d) =
-      u32x2{pack_bf16x2(num[0], num[1]), pack_bf16x2(num[2], num[3])};
-  if (d == 0 && a.lse) a.lse[q] = den == 0.f ? -INFINITY : (M + __log2f(den)) * kLn2;
+  write_row(a, q, d, D, num, M, den);
+}
+
+// Joins the key ranges of the tiles that have more than one: a thread takes 4 dims of a
+// row, a workgroup the rows that its threads make.
+template <int D>
+constexpr int merge_rows() { return kApThreads / (D / 4); }
+
+template <int D>
+__global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
+  const int g = blockIdx.x % a.Hkv;
+  const int rest = blockIdx.x / a.Hkv;
+  constexpr int kParts = kP4Rows / merge_rows<D>();
+  const int4 e = a.tiles[rest / kParts];
+  const int r0 = e.x, row0 = e.y, rows = e.z, n = e.w;
+  const int row = rest % kParts * merge_rows<D>() + threadIdx.x / (D / 4);
+  const int d = 4 * (threadIdx.x % (D / 4));
+  if (n == 1 || row >= rows) return;
+  const int at = row0 + row;
+  const int64_t q = static_cast<int64_t>(r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
+  merge_row<D>(a, q, d, n);
+}
+
+// ---------------------------------------------------------------- few rows
+// Requests that bring few rows each (a token or a few behind a long context) leave most
+// of a 128-row tile empty, and their time is that of reading the cache: as in decode, one
+// wave (or two or four, whose results meet in LDS) takes 16 rows of a request and KV head
+// over a partition of up to 64 blocks, in its registers (kv4_attn.hpp). A request with
+// more rows takes several such units, which read the same blocks.
+constexpr int kFewRows = 16;
+
+// The slot-th tile of kFewRows rows: requests in order. Every lane returns the same;
+// false past the last.
+struct FewTile {
+  int b, r0, L;
+  int row0, rows;  // of the request's (token, query head of the group) rows
+  int prefix;      // cached tokens before the chunk
+  int first;       // position of the first row
+  int blocks;      // blocks that the last row sees
+};
+
+__device__ bool find_few(const Prefill4Args& a, int slot, FewTile* t) {
+  const int lane = threadIdx.x % kWave;
+  for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    int n = 0, r0 = 0, rows = 0, L = 0;
+    if (b0 + lane < a.B) {
+      r0 = a.q_indptr[b0 + lane];
+      const int r1 = a.q_indptr[b0 + lane + 1];
+      L = a.ctx_lens[b0 + lane];
+      if (rows_ok4(r0, r1, a.T)) rows = (r1 - r0) * a.group;
+      n = (rows + kFewRows - 1) / kFewRows;
+    }
+    int incl = n;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int up = __shfl_up(incl, off);
+      if (lane >= off) incl += up;
+    }
+    const uint64_t past = __ballot(incl > slot);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      rows = __builtin_amdgcn_readlane(rows, l);
+      t->b = b0 + l;
+      t->r0 = __builtin_amdgcn_readlane(r0, l);
+      t->L = __builtin_amdgcn_readlane(L, l);
+      t->row0 = (slot - __builtin_amdgcn_readlane(incl - n, l)) * kFewRows;
+      t->rows = min(kFewRows, rows - t->row0);
+      t->prefix = t->L - rows / a.group;
+      t->first = t->prefix + t->row0 / a.group;
+      const int last = t->prefix + (t->row0 + t->rows - 1) / a.group;
+      t->blocks = last < 0 ? 0 : min(last / kBlockSize + 1, a.max_blocks);
+      return true;
+    }
+    slot -= __builtin_amdgcn_readlane(incl, kWave - 1);
+  }
+  return false;
+}
+
+// Row r of a tile: token * Hq + query head.
+__device__ __forceinline__ int64_t few_row(const Prefill4Args& a, const FewTile& t, int g, int r) {
+  const int at = t.row0 + r;
+  return static_cast<int64_t>(t.r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
+}
+
+template <int D, int W>
+__global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
+  using L4 = Kv4<D>;
+  constexpr int DEPTH = 2;  // pairs of blocks in registers
+  const int lane = threadIdx.x % kWave, col = lane % 16, kgrp = lane / 16;
+  const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int g = blockIdx.x % a.Hkv;
+  const int rest = blockIdx.x / a.Hkv;
+  const int part = rest % a.ranges;
+  FewTile t;
+  if (!find_few(a, rest / a.ranges, &t)) return;
+  const int n_parts = max(1, (t.blocks + a.pb - 1) / a.pb);
+  if (part >= n_parts) return;
+  // Partitions count from the end, as in decode.
+  const int jend = t.blocks - part * a.pb, j0 = max(0, jend - a.pb);
+  const int32_t* table = a.block_table + static_cast<int64_t>(t.b) * a.max_blocks;
+  const int rv = a.req_version[t.b];
+  int my_phys = 0;
+  bool ok = false;
+  if (lane < a.pb && j0 + lane < jend) {
+    my_phys = table[j0 + lane];
+    ok = my_phys >= 0 && my_phys < a.num_blocks && a.block_version[my_phys] == rv;
+    if (!ok) my_phys = 0;  // an id outside the pool is never dereferenced
+  }
+  const uint64_t part_valid = __ballot(ok);
+  uint64_t valid = part_valid;
+  if (W > 1)
+    valid = __ballot(ok && __popcll(part_valid & ((1ull << lane) - 1ull)) % W == wave);
+
+  Attn4<D> at;
+  const bool in = col < t.rows;
+  at.load_q(a.q + (in ? few_row(a, t, g, col) : 0) * D, in, a.q_xor, a.q_and);
+  const float inv_scale = 1.f / a.scale_log2;
+  at.init(inv_scale);
+  const int pos = in ? t.prefix + (t.row0 + col) / a.group : INT_MAX - kBlockSize;
+
+  auto next_block = [&]() -> int {
+    if (!valid) return -1;
+    const int i = __builtin_ctzll(valid);
+    valid &= valid - 1;
+    return i;
+  };
+  // V of a block at the end of what is seen: slots past the context's end, and tokens that
+  // are not finite, as zeros; returns the latter for the group of this lane's output dims.
+  auto settle = [&](Regs4<D>& R, int e, int j) {
+    uint32_t odd = 0u, bad = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t byte = 0xffu << (8 * i);
+      const bool dead = j * kBlockSize + 4 * kgrp + i >= t.L, is = (R.vs[e] & byte) == byte;
+      if (is && !dead) odd |= 1u << i;
+      if (is || dead) {
+        R.vs[e] &= ~byte;
+        if constexpr (D == 128)
+          R.v[e][i] = 0u;
+        else
+          R.v[e][i / 2] &= ~(0xffffu << (16 * (i % 2)));
+      }
+    }
+    if (__ballot(odd != 0u)) {
+      const int from = L4::k_group(kgrp) * (16 / L4::kGroups);  // a column of the group
+      for (int kg = 0; kg < 4; ++kg) bad |= __shfl(odd, kg * 16 + from) << (4 * kg);
+    }
+    return bad;
+  };
+  auto compute = [&](Regs4<D>& R, int i0, int i1) {
+    f32x4 sc[2];
+    bool hit = false;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = e ? i1 : i0, j = j0 + i;
+      // a block that some row sees in part, or none
+      const bool tail = i < 0 || j * kBlockSize + kBlockSize - 1 > t.first;
+      const int seen = i < 0 ? 0 : min(max(pos - j * kBlockSize + 1, 0), kBlockSize);
+      if (tail && i >= 0) hit |= (settle(R, e, j) & ((1u << seen) - 1u)) != 0u;
+      sc[e] = at.scores(R, e);
+      if (tail) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[e][k] = 4 * kgrp + k < seen ? sc[e][k] : -INFINITY;
+      }
+    }
+    float ps[2];
+    u32x4 pf;
+    at.weigh(sc, a.scale_log2, inv_scale, ps, pf);
+    at.values(R, pf);
+    if (hit) {
+      const float nan = __builtin_nanf("");
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) at.acc[k] = f32x4{nan, nan, nan, nan};
+    }
+  };
+
+  Regs4<D> R[DEPTH];
+  int i0[DEPTH], i1[DEPTH];
+  auto fill = [&](int d) {
+    i0[d] = next_block();
+    i1[d] = next_block();
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = e ? i1[d] : i0[d];
+      const int p = i >= 0 ? __builtin_amdgcn_readlane(my_phys, i) : 0;
+      load_block4<D>(R[d], e, a.kv4, static_cast<int64_t>(p) * a.Hkv + g, i >= 0);
+    }
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH - 1; ++d) fill(d);
+  bool done = false;
+  while (!done) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      fill((d + DEPTH - 1) % DEPTH);
+      if (i0[d] < 0) {
+        done = true;
+        break;
+      }
+      compute(R[d], i0[d], i1[d]);
+    }
+  }
+
+  extern __shared__ __attribute__((aligned(16))) float mg[];
+  at.template finish<W>(t.rows, mg, [&](int r, int d, f32x4 num, float M, float den) {
+    const int64_t q = few_row(a, t, g, r);
+    if (n_parts == 1) {
+      write_row(a, q, d, D, num, M, den);
+    } else {
+      const int64_t to = q * a.ranges + part;
+      *reinterpret_cast<f32x4*>(a.part_o + to * D + d) = num;
+      if (d == 0) {
+        a.part_ml[2 * to] = M;
+        a.part_ml[2 * to + 1] = den;
+      }
+    }
+  });
+}
+
+template <int D>
+__global__ __launch_bounds__(kApThreads) void few_merge_kernel(Prefill4Args a) {
+  FewTile t;
+  if (!find_few(a, blockIdx.x / a.Hkv, &t)) return;
+  const int n = (t.blocks + a.pb - 1) / a.pb;
+  if (n <= 1) return;
+  for (int x = threadIdx.x; x < t.rows * (D / 4); x += kApThreads)
+    merge_row<D>(a, few_row(a, t, blockIdx.x % a.Hkv, x / (D / 4)), 4 * (x % (D / 4)), n);
+}
+
+template <int D>
+void launch_few(const Prefill4Args& a, unsigned grid, int W, hipStream_t s) {
+  const int lds = join4_bytes<D>(W, kFewRows);
+  if (W == 4)
+    few_kv4_kernel<D, 4><<<grid, 4 * kWave, lds, s>>>(a);
+  else if (W == 2)
+    few_kv4_kernel<D, 2><<<grid, 2 * kWave, lds, s>>>(a);
+  else
+    few_kv4_kernel<D, 1><<<grid, kWave, 0, s>>>(a);
 }
 
 template <int D>
 local_status_t launch_prefill_kv4(const Prefill4Args& a, hipStream_t s) {
   const char* who = "paged_attn_prefill_kv4";
   const int64_t units = static_cast<int64_t>(a.max_tiles) * a.ranges * a.Hkv;
-  const int64_t grid = std::min<int64_t>(units, kP4Units);
   // blocks that hold a chunk's tokens: at most one more than the chunk fills, each side
   const int64_t blocks = a.T / kBlockSize + 2 * static_cast<int64_t>(a.B);
   const int64_t append = 1 + (blocks * a.Hkv + kApWaves - 1) / kApWaves;
-  const int64_t merge = a.ranges > 1 ? static_cast<int64_t>(a.max_tiles) * (kP4Rows / merge_rows<D>()) * a.Hkv : 0;
+  const int64_t per_tile = a.pb ? 1 : kP4Rows / merge_rows<D>();
+  const int64_t merge = a.ranges > 1 ? a.max_tiles * per_tile * a.Hkv : 0;
   if (units >= (1LL << 31) || append >= (1LL << 31) || merge >= (1LL << 31))
     return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: %lld units, grids of %lld and %lld workgroups",
                       who, (long long)units, (long long)append, (long long)merge);
   if (a.k_new)
     append_kv4_kernel<D><<<static_cast<unsigned>(append), kApThreads, 0, s>>>(a);
-  else
+  else if (a.plan)
     plan_kv4_kernel<<<1, kApThreads, 0, s>>>(a);
-  prefill_kv4_kernel<D><<<static_cast<unsigned>(grid), kP4Threads, 0, s>>>(a);
-  if (merge) merge_kv4_kernel<D><<<static_cast<unsigned>(merge), kApThreads, 0, s>>>(a);
+  if (a.pb) {
+    launch_few<D>(a, static_cast<unsigned>(units), units < 1536 ? 4 : units < 5120 ? 2 : 1, s);
+    if (merge) few_merge_kernel<D><<<static_cast<unsigned>(merge), kApThreads, 0, s>>>(a);
+  } else {
+    const int64_t grid = std::min<int64_t>(units, kP4Units);
+    prefill_kv4_kernel<D><<<static_cast<unsigned>(grid), kP4Threads, 0, s>>>(a);
+    if (merge) merge_kv4_kernel<D><<<static_cast<unsigned>(merge), kApThreads, 0, s>>>(a);
+  }
   return local_check_launch(who);
 }
+
+// Calls of at most this many rows a request, on average, go by 16 rows. Measured in us by
+// 16 rows / by 128, 8 KV heads of 4 query heads, 8 requests behind 500 to 8000 tokens: 16
+// rows 28 / 42, 32 rows 37 / 41, 64 rows 49 / 42; 32 KV heads, 4 requests behind 100 to
+// 2000: 16 rows 21 / 31, 32 rows 26 / 31, 64 rows 33 / 32.
+constexpr int kFewMeanRows = 32;
 
 // Key ranges that a tile of a call may be split into: as many as give every compute unit
 // a workgroup where there are few tiles, counted from the sizes that the host knows.
 int ranges_of_call(int64_t tiles, int Hkv, int max_blocks) {
+  if (tiles == 0) return 1;
   const int64_t want = (2 * kP4Units + tiles * Hkv - 1) / (tiles * Hkv);
   const int64_t most = std::max(1, max_blocks / kP4MinRange);
   return static_cast<int>(std::min<int64_t>({want, most, kP4MaxRanges}));
@@ -937,15 +1180,22 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   if ((k_new == nullptr) != (v_new == nullptr))
     return local_fail(LOCAL_ERR_NULL, "%s: k_new and v_new must both be set", who);
   Prefill4Args a{};
+  const int64_t all_rows = T * (Hq / Hkv);
+  const bool few = all_rows <= static_cast<int64_t>(B) * kFewMeanRows;
   // (B tiles more than the rows fill: each request's last one)
-  const int64_t tiles = T * (Hq / Hkv) / kP4Rows + B;
+  const int64_t tiles = all_rows / (few ? kFewRows : kP4Rows) + B;
   if (tiles * kP4MaxRanges >= (1LL << 31))
     return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: T=%lld B=%d", who, (long long)T, B);
   a.max_tiles = static_cast<int>(tiles);
-  a.ranges = B > 0 && T > 0 ? ranges_of_call(tiles, Hkv, max_blocks) : 1;
+  if (few) {
+    a.pb = part_blocks(max_blocks, tiles * Hkv);
+    a.ranges = parts_of_table(max_blocks, a.pb);
+  } else {
+    a.ranges = ranges_of_call(tiles, Hkv, max_blocks);
+  }
   const size_t rows = static_cast<size_t>(T) * Hq * (a.ranges > 1 ? a.ranges : 0);
-  const size_t tiles_at = sizeof(Unit4) * tiles * a.ranges;
-  const size_t part_at = round256(tiles_at + sizeof(int4) * tiles);
+  const size_t tiles_at = few ? 0 : sizeof(Unit4) * tiles * a.ranges;
+  const size_t part_at = few ? 0 : round256(tiles_at + sizeof(int4) * tiles);
   const size_t need = part_at + rows * (D + 2) * sizeof(float);
   if (!ws) {
     *ws_bytes = need;
@@ -973,8 +1223,8 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   a.out = out;
   a.lse = lse;
   char* base = static_cast<char*>(ws);
-  a.plan = reinterpret_cast<int4*>(base);
-  a.tiles = reinterpret_cast<int4*>(base + tiles_at);
+  a.plan = few ? nullptr : reinterpret_cast<int4*>(base);
+  a.tiles = few ? nullptr : reinterpret_cast<int4*>(base + tiles_at);
   a.part_o = reinterpret_cast<float*>(base + part_at);
   a.part_ml = a.part_o + rows * D;
   a.T = T;

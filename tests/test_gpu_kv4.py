@@ -257,6 +257,12 @@ PREFILL = [
     ([4500], [20], 2, 2, 64, {}),
     ([0], [300], 2, 1, 128, {}),
     ([20], [30], 4, 2, 64, dict(width=2)),  # longer than its table
+    # few rows a request: 16 at a time
+    ([1700, 5, 900, 64], [2, 5, 1, 0], 16, 4, 128, dict(stale=0.2)),
+    ([700], [4], 16, 1, 64, {}),
+    ([2000, 100, 0], [3, 40, 16], 8, 8, 128, dict(stale=0.1)),
+    ([90, 40], [3, 2], 9, 3, 64, dict(all_stale=(1,), width=9)),
+    ([30], [4], 8, 2, 128, dict(width=2)),  # longer than its table
 ]
 
 
@@ -290,6 +296,27 @@ def test_prefill_of_many_requests():
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("prefix", [0, 700])
+def test_few_rows_of_values_that_are_not_finite(D, prefix):
+    """The same of 14 tokens (28 rows), and a slot past the context's end that holds NaN."""
+    c = Case(22, [prefix + 14], 4, 2, D, new=[14])
+    c.vn[5, 0, D - 1] = 0x7fc0    # V of token 5, KV head 0, the last group
+    c.vn[9, 1, 2] = 0xff80
+    c.kn[12, 1, 0] = 0x7f80       # K of token 12
+    nan = np.full((1, 2, D), np.nan)
+    last = prefix + 14
+    kv4.write(c.tiles, nan, nan, [c.table[0, last // BS]], [last % BS])
+    q, pool, meta, new = c.gpu()
+    want = c.appended()
+    ref, ref_lse, size, _ = c.ref(want)
+    assert not np.isnan(ref[:5]).any() and np.isnan(ref[5, :2, D - 32:]).all()
+    assert not np.isnan(ref[5, :2, :D - 32]).any()
+    assert not np.isnan(ref_lse[:12]).any() and np.isnan(ref_lse[12:, 2:]).all()
+    out, lse = lk.local_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, c.sm, **new)
+    check_out(out, lse, ref, ref_lse, size, "out")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("prefix", [0, 700])
 def test_prefill_of_values_that_are_not_finite(D, prefix):
     """A token whose K or V is not finite reaches the rows that see it and no other."""
     c = Case(21, [prefix + 60], 4, 2, D, new=[60])
@@ -306,13 +333,14 @@ def test_prefill_of_values_that_are_not_finite(D, prefix):
     check_out(out, lse, ref, ref_lse, size, "out")
 
 
-def test_prefill_skips_malformed_rows():
-    c = Case(31, [40, 50, 20], 4, 2, 64, new=[10, 20, 5])
+@pytest.mark.parametrize("hq", [2, 8])  # 16 rows at a time, 128 rows
+def test_prefill_skips_malformed_rows(hq):
+    c = Case(31, [40, 50, 20], hq, 2, 64, new=[10, 20, 5])
     q, pool, meta, new = c.gpu()
     starts = c.starts.copy()
     starts[2:] = [30, 400]   # the last request's rows end past T: skipped whole
     out, lse = (torch.full(s, 7.0, dtype=t, device="cuda")
-                for s, t in (((35, 4, 64), torch.bfloat16), ((35, 4), torch.float32)))
+                for s, t in (((35, hq, 64), torch.bfloat16), ((35, hq), torch.float32)))
     want = c.appended()
     ref, ref_lse, size, _ = c.ref(want)
     lk.local_paged_attn_prefill_kv4(q, dev(starts), pool, *meta, c.sm, out=out, lse=lse, **new)
@@ -323,11 +351,12 @@ def test_prefill_skips_malformed_rows():
     assert np.array_equal(pool.cpu().numpy(), want)
 
 
-def test_blocks_past_32_bits():
+@pytest.mark.parametrize("new", [[30, 60], [3, 7]])
+def test_blocks_past_32_bits(new):
     """A pool of more than 2^32 bytes: blocks at its far end."""
     hkv, D = 8, 128
     n = 2 ** 32 // (hkv * 17 * D) + 200
-    c = Case(41, [90, 200], 8, hkv, D, new=[30, 60])
+    c = Case(41, [90, 200], 8, hkv, D, new=new)
     far = n - 1 - np.arange(c.num)
     pool = torch.zeros((n, hkv, 17 * D), dtype=torch.uint8, device="cuda")
     pool[torch.from_numpy(far)] = torch.from_numpy(c.tiles).to("cuda")

@@ -79,6 +79,10 @@ def test_workspace_sizes(lib):
     a = lambda v: (v + 255) // 256 * 256  # noqa: E731
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4), None, ctypes.byref(n), None) == OK
     assert n.value == a(48 * 7 * 8 + 16 * 7) + 100 * 32 * 8 * 130 * 4
+    # few rows a request: partitions of 16 blocks, no plan
+    assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, T=4), None, ctypes.byref(n),
+                                            None) == OK
+    assert n.value == 4 * 32 * 4 * 130 * 4
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, T=1 << 20), None, ctypes.byref(n),
                                             None) == OK
     assert n.value == a(64 * ((1 << 15) + 4))
