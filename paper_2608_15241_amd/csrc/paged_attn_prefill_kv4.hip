@@ -46,8 +46,6 @@ constexpr int kP4MaxRanges = 16;
 constexpr int kP4Units = 256;                          // a workgroup for every compute unit
 constexpr int kApThreads = 256;                        // of the append launch
 constexpr int kApWaves = kApThreads / kWave;
-constexpr float kP4NegBig = -1.0e30f;
-constexpr float kP4Lazy = 8.f;  // log2 of the largest weight before the maximum rises
 
 struct Prefill4Args {
   const uint16_t* q;
@@ -117,6 +115,7 @@ constexpr int kPlanChoices = 3;
 
 __device__ void plan_kv4(const Prefill4Args& a) {
   __shared__ int4 cache[kPlanCache];
+  __shared__ int4 req[kApThreads];  // first token, tokens, context length, version
   __shared__ int first[kApThreads + 1], wave_sums[kApWaves], hist[256], longest;
   __shared__ int n_units[kPlanChoices];
   __shared__ unsigned long long work;
@@ -129,6 +128,7 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     int n = 0;
     if (b0 + tid < a.B) {
       const int r0 = a.q_indptr[b0 + tid], r1 = a.q_indptr[b0 + tid + 1];
+      req[tid] = int4{r0, r1 - r0, a.ctx_lens[b0 + tid], a.req_version[b0 + tid]};
       if (rows_ok4(r0, r1, a.T)) n = ((r1 - r0) * a.group + kP4Rows - 1) / kP4Rows;
     }
     const int incl = scan_ap(n, wave_sums);
@@ -138,7 +138,7 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     const int all = first[kApThreads];
     // (a plan is sized for row ranges that do not overlap)
     for (int t = tid; t < all && n_tiles + t < a.max_tiles; t += kApThreads) {
-      int lo = 0, hi = kApThreads;
+      int lo = 0, hi = min(a.B - b0, kApThreads);
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (first[mid] <= t)
@@ -147,7 +147,7 @@ __device__ void plan_kv4(const Prefill4Args& a) {
           hi = mid;
       }
       const int b = b0 + lo, row0 = (t - first[lo]) * kP4Rows, at = n_tiles + t;
-      const int blocks = blocks_of(a, a.q_indptr[b + 1] - a.q_indptr[b], a.ctx_lens[b], row0);
+      const int blocks = blocks_of(a, req[lo].y, req[lo].z, row0);
       const int4 e = {b, row0, blocks, 0};
       if (at < kPlanCache)
         cache[at] = e;
@@ -212,8 +212,15 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     }
     const int4 e = entry(t);
     const int b = e.x, row0 = e.y, blocks = e.z, n = ranges_of(blocks, inv_len);
-    const int r0 = a.q_indptr[b], tokens = a.q_indptr[b + 1] - r0, L = a.ctx_lens[b];
-    const int rows = min(kP4Rows, tokens * a.group - row0), rv = a.req_version[b];
+    int4 q;
+    if (a.B <= kApThreads) {
+      q = req[b];
+    } else {  // (only the last requests are still in LDS)
+      const int r0 = a.q_indptr[b];
+      q = int4{r0, a.q_indptr[b + 1] - r0, a.ctx_lens[b], a.req_version[b]};
+    }
+    const int r0 = q.x, tokens = q.y, L = q.z, rv = q.w;
+    const int rows = min(kP4Rows, tokens * a.group - row0);
     a.tiles[t] = int4{r0, row0, rows, n};
     const int at = atomicAdd(&hist[bucket(blocks, n)], n);
     for (int r = 0; r < n; ++r) {
@@ -586,7 +593,7 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
         const float alpha = fast_exp2(m_run[r] - m_new);
         l_run[r] *= alpha;
         m_run[r] = m_new;
-        rise[r] = (m_new + kP4Lazy) * inv_scale;
+        rise[r] = (m_new + kLazy4) * inv_scale;
 #pragma unroll
         for (int t = 0; t < VT; ++t) acc[r][t] *= alpha;
       }
@@ -753,9 +760,9 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   for (;;) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      m_run[r] = kP4NegBig;
+      m_run[r] = kNegBig4;
       l_run[r] = 0.f;
-      rise[r] = (kP4NegBig + kP4Lazy) * inv_scale;
+      rise[r] = (kNegBig4 + kLazy4) * inv_scale;
 #pragma unroll
       for (int t = 0; t < VT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -846,7 +853,7 @@ __device__ __forceinline__ void merge_row(const Prefill4Args& a, int64_t q, int 
   const float* po = a.part_o + q * a.ranges * D + d;
   // every range's loads in flight at once, 8 at a time
   constexpr int kBatch = 8;
-  float M = kP4NegBig, den = 0.f;
+  float M = kNegBig4, den = 0.f;
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   for (int p = 0; p < n; p += kBatch) {
     float2 m[kBatch];
