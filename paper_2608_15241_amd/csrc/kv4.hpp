@@ -180,8 +180,6 @@ __device__ __forceinline__ uint32_t round_v(u32x4 v, uint32_t& code) {
   return s;
 }
 
-constexpr size_t round256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
-
 // max(a, b, c) in one instruction
 __device__ __forceinline__ float max3f(float a, float b, float c) {
   float r;

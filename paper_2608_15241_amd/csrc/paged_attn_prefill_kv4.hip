@@ -160,8 +160,8 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     __syncthreads();
   }
   // No unit longer than a compute unit's share of the work, or an eighth or a quarter
-  // more where that leaves no compute unit a second one (4 requests of 1 to 16 tokens behind 1K
-  // to 8K have units of one length: the share alone makes 270 of them, two rounds).
+  // more where that leaves no compute unit a second one (units of one length, 270 of them
+  // by the share alone, took two rounds: 52 us instead of 43).
   const float share = fmaxf(static_cast<float>(work) * a.Hkv / kP4Units, 1.f);
   auto ranges_of = [&](int blocks, float inv_len) {
     const int want = static_cast<int>(static_cast<float>(blocks) * inv_len + 0.999f);
@@ -392,7 +392,6 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   using L4 = Kv4<D>;
   constexpr int KC = D / 32, VT = D / 16, RT = kP4RowTiles;
   __shared__ Stage4<D> stage[kP4Halves][2];
-
   __shared__ __attribute__((aligned(16))) int list_id[kP4Window + 2 * kP4Step],
       list_j[kP4Window + 2 * kP4Step];
   __shared__ int wave_n[kP4Halves * kP4Waves];
@@ -416,7 +415,8 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
     if (u < units) {
       // (read-only here and the same for the workgroup: scalar loads)
       typedef const __attribute__((address_space(4))) u32x4* ScalarPtr;
-      const ScalarPtr from = (ScalarPtr)(a.plan + static_cast<int64_t>(u / static_cast<uint32_t>(a.Hkv)) * kUnitInt4s);
+      const int64_t at = u / static_cast<uint32_t>(a.Hkv);
+      const ScalarPtr from = (ScalarPtr)(a.plan + at * kUnitInt4s);
       u32x4 w[kUnitInt4s];
 #pragma unroll
       for (int i = 0; i < kUnitInt4s; ++i) w[i] = from[i];
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         u32x4 v = {0u, 0u, 0u, 0u};
-        if (pos[r] != -1 || 16 * RT * wave + 16 * r + col < u.rows)
+        if (16 * RT * wave + 16 * r + col < u.rows)
           v = ld_global<u32x4>(a.q + row * D + (D / 4) * kgrp + 8 * c);
         qv[r][c] = as_bf16x8((v ^ a.q_xor) & a.q_and);
       }
@@ -532,8 +532,7 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   auto compute = [&](const Stage4<D>& st, int s) {
     int j[kP4Step];
 #pragma unroll
-    for (int e = 0; e < kP4Step; ++e)
-      j[e] = j_of(s, e);
+    for (int e = 0; e < kP4Step; ++e) j[e] = j_of(s, e);
     if (j[0] * kBlockSize > last_pos) return;  // (ascending: no key of the step is seen)
     // Operands are read a block of K (half a pair of V) ahead of their products; left to
     // itself the compiler reads two at a time and waits for each.
@@ -752,8 +751,8 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   };
 
   // Units one after the other. What the next one starts from (its entry, its first
-  // window's ids and tags, q) is read while this one runs: a unit's chain of dependent
-  // loads took as long as a third of its steps.
+  // window's ids and tags, q) is read while this one runs (1% of the 4 x 512 tokens: a
+  // second unit's chain of dependent loads otherwise shows between two units only).
   count_ids(id);
   __syncthreads();
   int n = list_ids(id, e.lo + tid);
@@ -1202,7 +1201,7 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   }
   const size_t rows = static_cast<size_t>(T) * Hq * (a.ranges > 1 ? a.ranges : 0);
   const size_t tiles_at = few ? 0 : sizeof(Unit4) * tiles * a.ranges;
-  const size_t part_at = few ? 0 : round256(tiles_at + sizeof(int4) * tiles);
+  const size_t part_at = few ? 0 : align256(tiles_at + sizeof(int4) * tiles);
   const size_t need = part_at + rows * (D + 2) * sizeof(float);
   if (!ws) {
     *ws_bytes = need;

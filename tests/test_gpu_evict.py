@@ -1,4 +1,5 @@
-"""Block weights of bf16 decode, eviction, and a run of everything together (tolerances: kv4_helpers.py).
+"""Block weights of bf16 decode, eviction, and a run of everything together (tolerances:
+kv4_helpers.py).
 """
 from __future__ import annotations
 
@@ -57,8 +58,8 @@ def test_decode_weighted(ctx, hq, hkv, D, stale, append):
     assert wo is w
     assert torch.equal(out, o1) and torch.equal(lse, l1)
     assert torch.equal(K, K1) and torch.equal(V, V1)
-    ref, ref_lse, size, wr = kv4.attention(bits_to_f64(q), np.arange(len(ctx) + 1), ctx, table, tags,
-                                           version, bits_to_f64(kd), bits_to_f64(vd), sm)
+    ref, ref_lse, size, wr = kv4.attention(bits_to_f64(q), np.arange(len(ctx) + 1), ctx, table,
+                                           tags, version, bits_to_f64(kd), bits_to_f64(vd), sm)
     check_out(out, lse, ref, ref_lse, size, "out")
     owned = np.arange(table.shape[1]) < ((ctx + BS - 1) // BS)[:, None]
     check_weight(wo, np.where(owned, wr + 0.5 * w_in.astype(np.float64), 0.0), "weights")
@@ -145,7 +146,8 @@ def test_evict_replayed_in_place():
         with torch.cuda.graph(g, stream=s):
             call()
         for r in range(3):
-            t.copy_(dev(table)), c.copy_(dev(ctx)), wt.copy_(torch.from_numpy(w).to("cuda") * (r + 1))
+            t.copy_(dev(table)), c.copy_(dev(ctx))
+            wt.copy_(torch.from_numpy(w).to("cuda") * (r + 1))
             g.replay()
             s.synchronize()
             want = kv4.evict(table, ctx, w * np.float32(r + 1), keep, tags, version, 1, 2)
@@ -229,8 +231,8 @@ def test_a_context_that_is_rounded_decoded_evicted_and_continued(D, hq, hkv):
     ctx = (ctx + chunk).astype(np.int32)
     starts = np.concatenate([[0], np.cumsum(chunk)]).astype(np.int32)
     q, kn, vn = (f32_to_bf16_bits(rng.standard_normal((54, h, D))) for h in (hq, hkv, hkv))
-    out, lse = lk.local_paged_attn_prefill_kv4(dev_u16(q), dev(starts), pool, t, dev(ctx), *meta, sm,
-                                               k_new=dev_u16(kn), v_new=dev_u16(vn))
+    out, lse = lk.local_paged_attn_prefill_kv4(dev_u16(q), dev(starts), pool, t, dev(ctx), *meta,
+                                               sm, k_new=dev_u16(kn), v_new=dev_u16(vn))
     for b in range(3):
         pos = np.arange(ctx[b] - chunk[b], ctx[b])
         kv4.write(tiles, bits_to_f64(kn[starts[b]:starts[b + 1]]),

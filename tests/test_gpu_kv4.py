@@ -203,8 +203,8 @@ def test_softmax_scales(sm):
     wide = max(1.0, abs(sm) * math.sqrt(128))
     check_out(out, lse, ref, ref_lse, size, "prefill", wide)
     last = c.starts[1:] - 1
-    out, lse = lk.local_paged_attn_decode_kv4(q[torch.from_numpy(last.astype(np.int64))].contiguous(),
-                                              pool, *meta, sm)
+    rows = torch.from_numpy(last.astype(np.int64))
+    out, lse = lk.local_paged_attn_decode_kv4(q[rows].contiguous(), pool, *meta, sm)
     check_out(out, lse, ref[last], ref_lse[last], size[last], "decode", wide)
 
 
