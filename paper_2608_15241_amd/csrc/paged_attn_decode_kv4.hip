@@ -53,43 +53,44 @@ __global__ __launch_bounds__(kWave* W, 3) void decode_kv4_kernel(DecodeArgs a, i
   const int lane = threadIdx.x % kWave;
   const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane % 16, kgrp = lane / 16;
-  // Units and their order: as decode_attn_kernel.
+  // Ranked units and their order: as decode_attn_kernel, partitions counted from the end.
+  // Otherwise partition p is blocks [pb p, pb (p + 1)), so that the table's entries are
+  // on their way before the length is known.
   const int g = blockIdx.x % a.Hkv;
   const int slot = blockIdx.x / a.Hkv;
-  int b, part;
-  if (RANKED) {
+  int b, part, L, nb, n_full, j0, jend;
+  int my_phys = -1;
+  const int32_t* table = a.block_table;
+  if constexpr (RANKED) {
     b = decode_unit(a, B, slot, &part);
     if (b < 0) return;
+    L = a.ctx_lens[b];
+    nb = owned_blocks(L, a.max_blocks);
+    n_full = full_parts(nb, a.pb);
+    jend = nb - part * a.pb;
+    j0 = max(0, jend - a.pb);
+    table += static_cast<int64_t>(b) * a.max_blocks;
+    if (lane < a.pb && j0 + lane < jend) my_phys = table[j0 + lane];
   } else {
     b = slot % B;
     part = slot / B;
+    L = a.ctx_lens[b];
+    j0 = part * a.pb;
+    table += static_cast<int64_t>(b) * a.max_blocks;
+    if (lane < a.pb && j0 + lane < a.max_blocks) my_phys = table[j0 + lane];
+    nb = owned_blocks(L, a.max_blocks);
+    if (j0 >= max(nb, 1)) return;
+    n_full = full_parts(nb, a.pb);
+    jend = min(nb, j0 + a.pb);
   }
-  const int L = a.ctx_lens[b];
-  const int nb = owned_blocks(L, a.max_blocks);
-  const int n_full = full_parts(nb, a.pb), rem = nb - n_full * a.pb;
-  if (!RANKED) {
-    if (part < a.n_parts) {
-      if (part >= n_full && !(nb == 0 && part == 0)) return;
-    } else {
-      if (rem == 0) return;
-      part = n_full;
-    }
-  }
-  const int jend = nb - part * a.pb;
-  const int j0 = max(0, jend - a.pb);
-  const int n_parts_b = max(1, n_full + (rem > 0 ? 1 : 0));
+  const int n_parts_b = max(1, n_full + (nb > n_full * a.pb ? 1 : 0));
   const int rv = a.req_version[b];
-  const int32_t* table = a.block_table + static_cast<int64_t>(b) * a.max_blocks;
   const int G = a.group;
 
   const bool owned = lane < a.pb && j0 + lane < jend;
-  int my_phys = 0;
   bool ok = false;
-  if (owned) {
-    my_phys = table[j0 + lane];
-    ok = my_phys >= 0 && my_phys < a.num_blocks && a.block_version[my_phys] == rv;
-    if (!ok) my_phys = 0;  // an id outside the pool is never dereferenced
-  }
+  if (owned) ok = my_phys >= 0 && my_phys < a.num_blocks && a.block_version[my_phys] == rv;
+  if (!ok) my_phys = 0;  // an id outside the pool is never dereferenced
   const uint64_t part_valid = __ballot(ok);
   uint64_t valid_mask = part_valid;
   if (W > 1)
@@ -281,11 +282,13 @@ local_status_t launch_decode_kv4(const DecodeArgs& a, int B, hipStream_t s) {
   if (std::max(wgs, merge) >= (1LL << 31))
     return local_fail(LOCAL_ERR_UNSUPPORTED, "paged_attn_decode_kv4: grid of %lld workgroups",
                       (long long)std::max(wgs, merge));
-  const unsigned grid = static_cast<unsigned>(wgs);
   const int W = kv4_waves(a, B);
-  // (units that are all resident at once need no order, and finding it takes a call of
-  // 4 requests 1 us of 6.7)
-  const bool ranked = B <= kRankChunks * kWave && wgs * W > 2048;
+  // (units that are about all resident at once need no order, and finding it takes a call
+  // of 4 requests 1 us of 6.7; 128 short requests, 4096 waves, 15.4 us with and 14.1
+  // without, 16 of up to 4000 tokens, 4352 waves, 18.0 with and 18.7 without)
+  const bool ranked = B <= kRankChunks * kWave && wgs * W > 4096;
+  const unsigned grid =
+      static_cast<unsigned>(a.Hkv) * B * static_cast<unsigned>(a.n_parts + (ranked ? 1 : 0));
   if (ranked)
     a.w_out ? launch_kv4<D, true, true>(a, B, grid, W, s)
             : launch_kv4<D, true, false>(a, B, grid, W, s);
