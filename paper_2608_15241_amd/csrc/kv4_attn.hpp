@@ -100,7 +100,8 @@ struct Attn4 {
   __device__ __forceinline__ void weigh(const f32x4 (&sc)[2], float scale, float inv_scale,
                                         float (&ps)[2], u32x4& pf) {
     const float mx = max3f(max3f(sc[0][0], sc[0][1], sc[0][2]),
-                           max3f(sc[0][3], sc[1][0], sc[1][1]), max2f(sc[1][2], sc[1][3]));
+                           max3f(sc[0][3], sc[1][0], sc[1][1]),
+                           __builtin_elementwise_maximum(sc[1][2], sc[1][3]));
     if (__ballot(mx > rise)) {
       const float m_new = fmaxf(m_run, max_xor32(max_xor16(mx)) * scale);
       const float alpha = fast_exp2(m_run - m_new);

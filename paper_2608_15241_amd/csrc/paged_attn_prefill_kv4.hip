@@ -586,7 +586,7 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
       mx = max3f(mx, sc[r][2][1], sc[r][2][2]);
       mx = max3f(mx, sc[r][2][3], sc[r][3][0]);
       mx = max3f(mx, sc[r][3][1], sc[r][3][2]);
-      mx = max2f(mx, sc[r][3][3]);
+      mx = __builtin_elementwise_maximum(mx, sc[r][3][3]);
       if (__ballot(mx > rise[r])) {
         const float m_new = fmaxf(m_run[r], max_xor32(max_xor16(mx)) * a.scale_log2);
         const float alpha = fast_exp2(m_run[r] - m_new);

@@ -376,6 +376,30 @@ def test_blocks_past_32_bits(new):
     check_out(out, lse, ref[last], ref_lse[last], size[last], "decode")
 
 
+# 16 rows at a time: a long request of few rows, several; 128 rows
+@pytest.mark.parametrize("prefix,chunk,hq,hkv,D", [
+    ([767, 0], [8, 4], 8, 2, 128), ([900, 30, 500], [5, 2, 20], 2, 2, 64),
+    ([700, 41], [90, 300], 8, 2, 128), ([4500], [200], 4, 4, 64)])
+def test_results_repeat(prefix, chunk, hq, hkv, D):
+    """Calls of the same inputs return the same bits."""
+    ctx = np.array(prefix) + np.array(chunk)
+    c = Case(71, ctx, hq, hkv, D, new=chunk, stale=0.1)
+    q, pool, meta, new = c.gpu()
+    last = torch.from_numpy(c.starts[1:].astype(np.int64) - 1).to("cuda")
+    w = torch.zeros(c.table.shape, device="cuda")
+
+    def call():
+        pre = lk.local_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, c.sm, **new)
+        dec = lk.local_paged_attn_decode_kv4(q[last], pool, *meta, c.sm, weight_in=w,
+                                             weight_out=torch.zeros_like(w), weight_decay=0.0)
+        return pre + dec
+
+    first = call()
+    for r in range(30):
+        for a, b in zip(call(), first):
+            assert torch.equal(a, b), r
+
+
 def test_replays_and_streams():
     """A captured decode and prefill of one workspace, replayed between eager work, on a
     stream that is not the default one."""
