@@ -1149,7 +1149,19 @@ local_status_t launch_prefill_kv4(const Prefill4Args& a, hipStream_t s) {
 // 16 rows / by 128, 8 KV heads of 4 query heads, 8 requests behind 500 to 8000 tokens: 16
 // rows 28 / 42, 32 rows 37 / 41, 64 rows 49 / 42; 32 KV heads, 4 requests behind 100 to
 // 2000: 16 rows 21 / 31, 32 rows 26 / 31, 64 rows 33 / 32.
+//
+// So do calls of more rows whose 16-row tiles, times KV heads, times entries of a request's
+// table (a bound on the blocks that they unpack) are at most this: the plan and the 128-row
+// workgroups' start and joins outlast their steps there. Over 60 calls of 1 to 8 requests
+// with 1 to 700 new tokens: 16 rows take 0.67 to 0.91 of the time of 128 up to 8000, 0.65
+// to 1.15 between 8000 and 16384 (two of thirteen above 1.02), 0.72 to 1.32 beyond.
 constexpr int kFewMeanRows = 32;
+constexpr int64_t kFewWork = 16384;
+
+bool few_rows(int64_t all_rows, int B, int Hkv, int max_blocks) {
+  return all_rows <= static_cast<int64_t>(B) * kFewMeanRows ||
+         all_rows / kFewRows + B <= kFewWork / max_blocks / Hkv;
+}
 
 // Key ranges that a tile of a call may be split into: as many as give every compute unit
 // a workgroup where there are few tiles, counted from the sizes that the host knows.
@@ -1187,7 +1199,7 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
     return local_fail(LOCAL_ERR_NULL, "%s: k_new and v_new must both be set", who);
   Prefill4Args a{};
   const int64_t all_rows = T * (Hq / Hkv);
-  const bool few = all_rows <= static_cast<int64_t>(B) * kFewMeanRows;
+  const bool few = few_rows(all_rows, B, Hkv, max_blocks);
   // (B tiles more than the rows fill: each request's last one)
   const int64_t tiles = all_rows / (few ? kFewRows : kP4Rows) + B;
   if (tiles * kP4MaxRanges >= (1LL << 31))

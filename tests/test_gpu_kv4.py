@@ -59,6 +59,16 @@ class Case:
         self.kn, self.vn = (f32_to_bf16_bits(rng.standard_normal((T, hkv, D))) for _ in range(2))
         self.sm = 1.0 / math.sqrt(D)
 
+    def widen(self):
+        """A table as for the longest contexts, of garbage past these: with more than 32 rows
+        a request on average, attention then goes by 128 rows (the rule takes a table's width
+        for its contexts)."""
+        more = np.full((len(self.ctx), 17000), -3, np.int32)
+        more[:, :self.table.shape[1]] = self.table
+        if self.table.shape[1] < ((self.ctx + BS - 1) // BS).max():
+            raise ValueError("the contexts would no longer end with the table")
+        self.table = more
+
     def gpu(self, append=True):
         self.pool = torch.from_numpy(self.tiles.copy()).to("cuda")
         self.meta = [dev(x) for x in (self.table, self.ctx, self.tags, self.version)]
@@ -263,16 +273,20 @@ PREFILL = [
     ([2000, 100, 0], [3, 40, 16], 8, 8, 128, dict(stale=0.1)),
     ([90, 40], [3, 2], 9, 3, 64, dict(all_stale=(1,), width=9)),
     ([30], [4], 8, 2, 128, dict(width=2)),  # longer than its table
+    ([600, 3], [300, 90], 32, 32, 64, dict(stale=0.1)),
 ]
 
 
 @pytest.mark.parametrize("i", range(len(PREFILL)))
 @pytest.mark.parametrize("append", [True, False])
-def test_prefill(i, append):
+@pytest.mark.parametrize("wide", [True, False])
+def test_prefill(i, append, wide):
     prefix, chunk, hq, hkv, D, more = PREFILL[i]
     ctx = np.array(prefix) + np.array(chunk)
     c = Case(200 + i, ctx, hq, hkv, D, new=chunk, **more)
-    say("prefill", i, prefix, chunk, hq, hkv, D, "append", append)
+    if wide and more.get("width") != 2:
+        c.widen()
+    say("prefill", i, prefix, chunk, hq, hkv, D, "append", append, "wide", wide)
     q, pool, meta, new = c.gpu(append)
     want = c.appended() if append else c.tiles
     ref, ref_lse, size, _ = c.ref(want)
@@ -281,11 +295,13 @@ def test_prefill(i, append):
     assert np.array_equal(pool.cpu().numpy(), want)
 
 
-def test_prefill_of_many_requests():
+# 16 rows at a time, 128 rows (one range each)
+@pytest.mark.parametrize("most,hq,hkv", [(9, 32, 8), (90, 16, 16)])
+def test_prefill_of_many_requests(most, hq, hkv):
     """More requests than one scan of the tile search takes, in one range (many tiles)."""
     rng = np.random.default_rng(3)
-    prefix, chunk = rng.integers(0, 60, 140), rng.integers(0, 9, 140)
-    c = Case(4, prefix + chunk, 32, 8, 64, new=chunk, stale=0.1)
+    prefix, chunk = rng.integers(0, 60, 140), rng.integers(0, most, 140)
+    c = Case(4, prefix + chunk, hq, hkv, 64, new=chunk, stale=0.1)
     q, pool, meta, new = c.gpu()
     want = c.appended()
     ref, ref_lse, size, _ = c.ref(want)
@@ -317,9 +333,12 @@ def test_few_rows_of_values_that_are_not_finite(D, prefix):
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("prefix", [0, 700])
-def test_prefill_of_values_that_are_not_finite(D, prefix):
+@pytest.mark.parametrize("wide", [True, False])
+def test_prefill_of_values_that_are_not_finite(D, prefix, wide):
     """A token whose K or V is not finite reaches the rows that see it and no other."""
     c = Case(21, [prefix + 60], 4, 2, D, new=[60])
+    if wide:
+        c.widen()
     c.vn[25, 0, D - 1] = 0x7fc0   # V of token 25, KV head 0, the last group
     c.vn[40, 1, 2] = 0xff80
     c.kn[50, 1, 0] = 0x7f80       # K of token 50: the whole rows from there on
@@ -333,9 +352,11 @@ def test_prefill_of_values_that_are_not_finite(D, prefix):
     check_out(out, lse, ref, ref_lse, size, "out")
 
 
-@pytest.mark.parametrize("hq", [2, 8])  # 16 rows at a time, 128 rows
-def test_prefill_skips_malformed_rows(hq):
+@pytest.mark.parametrize("hq,wide", [(2, False), (8, False), (8, True)])
+def test_prefill_skips_malformed_rows(hq, wide):
     c = Case(31, [40, 50, 20], hq, 2, 64, new=[10, 20, 5])
+    if wide:  # 128 rows at a time
+        c.widen()
     q, pool, meta, new = c.gpu()
     starts = c.starts.copy()
     starts[2:] = [30, 400]   # the last request's rows end past T: skipped whole
@@ -351,12 +372,12 @@ def test_prefill_skips_malformed_rows(hq):
     assert np.array_equal(pool.cpu().numpy(), want)
 
 
-@pytest.mark.parametrize("new", [[30, 60], [3, 7]])
-def test_blocks_past_32_bits(new):
+@pytest.mark.parametrize("new,width", [([30, 60], None), ([30, 60], 17000), ([3, 7], None)])
+def test_blocks_past_32_bits(new, width):
     """A pool of more than 2^32 bytes: blocks at its far end."""
     hkv, D = 8, 128
     n = 2 ** 32 // (hkv * 17 * D) + 200
-    c = Case(41, [90, 200], 8, hkv, D, new=new)
+    c = Case(41, [90, 200], 8, hkv, D, new=new, width=width)
     far = n - 1 - np.arange(c.num)
     pool = torch.zeros((n, hkv, 17 * D), dtype=torch.uint8, device="cuda")
     pool[torch.from_numpy(far)] = torch.from_numpy(c.tiles).to("cuda")
@@ -400,10 +421,13 @@ def test_results_repeat(prefix, chunk, hq, hkv, D):
             assert torch.equal(a, b), r
 
 
-def test_replays_and_streams():
+@pytest.mark.parametrize("wide", [True, False])
+def test_replays_and_streams(wide):
     """A captured decode and prefill of one workspace, replayed between eager work, on a
     stream that is not the default one."""
     c = Case(51, [300, 41, 800], 8, 2, 128, new=[20, 1, 33], stale=0.1)
+    if wide:
+        c.widen()
     q, pool, meta, new = c.gpu()
     last = torch.from_numpy(c.starts[1:].astype(np.int64) - 1)
     ws = lk.Workspace()
