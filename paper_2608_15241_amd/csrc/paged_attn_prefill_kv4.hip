@@ -41,11 +41,21 @@ constexpr int kP4RowTiles = 2;                         // 16-row tiles of a wave
 constexpr int kP4Rows = kP4Waves * 16 * kP4RowTiles;   // rows of a workgroup
 constexpr int kP4Step = 4;                             // blocks a step
 constexpr int kP4Window = kP4Threads;                  // table entries listed at a time
-constexpr int kP4MinRange = 8;                         // blocks a key range has at least
+constexpr int kP4MinRange = 16;                        // blocks a key range has at least
 constexpr int kP4MaxRanges = 16;
 constexpr int kP4Units = 256;                          // a workgroup for every compute unit
 constexpr int kApThreads = 256;                        // of the append launch
 constexpr int kApWaves = kApThreads / kWave;
+
+// Blocks of a key range below which tiles (times KV heads) of this number are not cut
+// further. A range's partial result, 128 rows in float32, is written and read again, which
+// takes as long as some 24 blocks' products; with more tiles fewer compute units are idle
+// without it. Against ranges of 8 blocks or a compute unit's share, whichever is longer,
+// calls took 0.58 to 1.12 of the time, 0.92 to 0.93 on average over two sets of 40 (202
+// tiles of 1 to 31 blocks 39 -> 24 us); one bound for all, 24 or 48, 0.94.
+__host__ __device__ inline int least_range(int64_t units) {
+  return static_cast<int>(units < 4 * kP4MinRange ? kP4MinRange : units < 256 ? units / 4 : 64);
+}
 
 struct Prefill4Args {
   const uint16_t* q;
@@ -159,10 +169,11 @@ __device__ void plan_kv4(const Prefill4Args& a) {
     n_tiles = min(n_tiles + all, a.max_tiles);
     __syncthreads();
   }
-  // No unit longer than a compute unit's share of the work, or an eighth or a quarter
-  // more where that leaves no compute unit a second one (units of one length, 270 of them
+  // No unit longer than a compute unit's share of the work (and least_range), or an eighth
+  // or a quarter more where that leaves no compute unit a second one (units of one length, 270 of them
   // by the share alone, took two rounds: 52 us instead of 43).
-  const float share = fmaxf(static_cast<float>(work) * a.Hkv / kP4Units, 1.f);
+  const float share = fmaxf(static_cast<float>(work) * a.Hkv / kP4Units,
+                            least_range(static_cast<int64_t>(n_tiles) * a.Hkv));
   auto ranges_of = [&](int blocks, float inv_len) {
     const int want = static_cast<int>(static_cast<float>(blocks) * inv_len + 0.999f);
     return max(1, min(want, min(a.ranges, blocks / kP4MinRange)));
@@ -1151,12 +1162,12 @@ local_status_t launch_prefill_kv4(const Prefill4Args& a, hipStream_t s) {
 // 2000: 16 rows 21 / 31, 32 rows 26 / 31, 64 rows 33 / 32.
 //
 // So do calls of more rows whose 16-row tiles, times KV heads, times entries of a request's
-// table (a bound on the blocks that they unpack) are at most this: the plan and the 128-row
-// workgroups' start and joins outlast their steps there. Over 60 calls of 1 to 8 requests
-// with 1 to 700 new tokens: 16 rows take 0.67 to 0.91 of the time of 128 up to 8000, 0.65
-// to 1.15 between 8000 and 16384 (two of thirteen above 1.02), 0.72 to 1.32 beyond.
+// table (a bound on the blocks that they unpack) are at most kFewWork: the plan and the
+// 128-row workgroups' start and joins outlast their steps there. Over 140 calls of 1 to 8
+// requests with 1 to 700 new tokens, 16 rows take 0.60 to 1.03 of the time of 128 up to
+// 32768 (one of 115 longer, 1.15), 0.72 to 1.66 beyond.
 constexpr int kFewMeanRows = 32;
-constexpr int64_t kFewWork = 16384;
+constexpr int64_t kFewWork = 32768;
 
 bool few_rows(int64_t all_rows, int B, int Hkv, int max_blocks) {
   return all_rows <= static_cast<int64_t>(B) * kFewMeanRows ||
@@ -1168,7 +1179,8 @@ bool few_rows(int64_t all_rows, int B, int Hkv, int max_blocks) {
 int ranges_of_call(int64_t tiles, int Hkv, int max_blocks) {
   if (tiles == 0) return 1;
   const int64_t want = (2 * kP4Units + tiles * Hkv - 1) / (tiles * Hkv);
-  const int64_t most = std::max(1, max_blocks / kP4MinRange);
+  const int least = least_range(tiles * Hkv);
+  const int64_t most = std::max(1, (max_blocks + least / 2) / least);
   return static_cast<int>(std::min<int64_t>({want, most, kP4MaxRanges}));
 }
 
