@@ -1226,7 +1226,8 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   const size_t rows = static_cast<size_t>(T) * Hq * (a.ranges > 1 ? a.ranges : 0);
   const size_t tiles_at = few ? 0 : sizeof(Unit4) * tiles * a.ranges;
   const size_t part_at = few ? 0 : align256(tiles_at + sizeof(int4) * tiles);
-  const size_t need = part_at + rows * (D + 2) * sizeof(float);
+  // (never 0: a caller's allocation of nothing may be NULL, which asks for the size)
+  const size_t need = std::max<size_t>(part_at + rows * (D + 2) * sizeof(float), 256);
   if (!ws) {
     *ws_bytes = need;
     return LOCAL_OK;

@@ -74,11 +74,20 @@ def test_workspace_sizes(lib):
     plain = [v for k, v in WEIGHTED.items() if k not in ("wi", "decay", "wo")]
     assert lib.local_paged_attn_decode(*plain, None, ctypes.byref(m), None) == OK
     assert n.value == (m.value + 255) // 256 * 256 + 4 * 64 * 32 * 4
-    # few tiles of 128 rows (400 / 128 + 4 requests): up to 8 key ranges of at least 8
-    # blocks, (D + 2) floats a row and range, behind 48 bytes a unit and 16 a tile
+    # few tiles of 128 rows (1200 / 128 + 4 requests, 8 heads): key ranges of at least
+    # 104 / 4 = 26 blocks, so 2 of 64; (D + 2) floats a row and range, behind 48 bytes a unit
+    # and 16 a tile
     a = lambda v: (v + 255) // 256 * 256  # noqa: E731
+    assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, T=300), None, ctypes.byref(n),
+                                            None) == OK
+    assert n.value == a(48 * 13 * 2 + 16 * 13) + 300 * 32 * 2 * 130 * 4
+    # little work in all: partitions of 64 blocks, halved to 16, no plan
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4), None, ctypes.byref(n), None) == OK
-    assert n.value == a(48 * 7 * 8 + 16 * 7) + 100 * 32 * 8 * 130 * 4
+    assert n.value == 100 * 32 * 4 * 130 * 4
+    # one block a request: one partition, written as it is
+    assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, mb=1), None, ctypes.byref(n),
+                                            None) == OK
+    assert n.value == 256
     # few rows a request: partitions of 16 blocks, no plan
     assert lib.local_paged_attn_prefill_kv4(*_args(PREFILL4, T=4), None, ctypes.byref(n),
                                             None) == OK
