@@ -5,7 +5,9 @@
 // v_mfma_f32_16x16x32_bf16, then O^T += V^T P^T over their 32 keys. A score tile's
 // layout (lane: 4 keys of one row) is that of the value product's B operand, and the
 // pool's codes lie as the A operands do, so nothing crosses lanes but a row's maximum
-// when it rises and its sum at the end.
+// when it rises and its sum at the end. Scores, maximum, sum and output are float32; the
+// weights are rounded to bf16 for the value product (2^-8 of each at most), which the
+// matrix instruction needs, but enter the sum unrounded.
 #pragma once
 
 #include <type_traits>
