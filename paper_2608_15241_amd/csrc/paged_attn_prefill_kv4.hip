@@ -859,12 +859,12 @@ __device__ __forceinline__ void write_row(const Prefill4Args& a, int64_t q, int 
 }
 
 // Joins the n parts (key ranges) of dims d .. d + 3 of row q (token * Hq + query head).
-template <int D>
+template <int D, int kBatch>
 __device__ __forceinline__ void merge_row(const Prefill4Args& a, int64_t q, int d, int n) {
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml + q * a.ranges * 2);
   const float* po = a.part_o + q * a.ranges * D + d;
-  // every range's loads in flight at once, 8 at a time
-  constexpr int kBatch = 8;
+  // every part's loads in flight at once, kBatch at a time (up to 8 it stops at the last;
+  // 16 as branches would take 110 registers)
   float M = kNegBig4, den = 0.f;
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   for (int p = 0; p < n; p += kBatch) {
@@ -884,8 +884,8 @@ __device__ __forceinline__ void merge_row(const Prefill4Args& a, int64_t q, int 
     num *= f;
 #pragma unroll
     for (int r = 0; r < kBatch; ++r) {
-      if (p + r >= n) break;
-      const float w = fast_exp2(m[r].x - top);
+      if (kBatch <= 8 && p + r >= n) break;
+      const float w = kBatch <= 8 || p + r < n ? fast_exp2(m[r].x - top) : 0.f;
       den += m[r].y * w;
       num += o[r] * w;
     }
@@ -911,7 +911,7 @@ __global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
   if (n == 1 || row >= rows) return;
   const int at = row0 + row;
   const int64_t q = static_cast<int64_t>(r0 + at / a.group) * a.Hq + g * a.group + at % a.group;
-  merge_row<D>(a, q, d, n);
+  merge_row<D, 8>(a, q, d, n);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -1111,13 +1111,21 @@ __global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kApThreads) void few_merge_kernel(Prefill4Args a) {
+__global__ __launch_bounds__(kFewRows* D / 4) void few_merge_kernel(Prefill4Args a) {
   FewTile t;
   if (!find_few(a, blockIdx.x / a.Hkv, &t)) return;
   const int n = (t.blocks + a.pb - 1) / a.pb;
   if (n <= 1) return;
-  for (int x = threadIdx.x; x < t.rows * (D / 4); x += kApThreads)
-    merge_row<D>(a, few_row(a, t, blockIdx.x % a.Hkv, x / (D / 4)), 4 * (x % (D / 4)), n);
+  const int row = threadIdx.x / (D / 4);
+  if (row >= t.rows) return;
+  const int64_t q = few_row(a, t, blockIdx.x % a.Hkv, row);
+  // (8 and 16 at a time: one request of 8 tokens behind 4000 18.8 and 16.1 us, 5 requests
+  // of 56 to 242 tokens, of 2 or 3 partitions, 28.5 and 30.5)
+  const int d = 4 * (threadIdx.x % (D / 4));
+  if (n <= 8)
+    merge_row<D, 8>(a, q, d, n);
+  else
+    merge_row<D, 16>(a, q, d, n);
 }
 
 template <int D>
@@ -1149,7 +1157,8 @@ local_status_t launch_prefill_kv4(const Prefill4Args& a, hipStream_t s) {
     plan_kv4_kernel<<<1, kApThreads, 0, s>>>(a);
   if (a.pb) {
     launch_few<D>(a, static_cast<unsigned>(units), units < 1536 ? 4 : units < 5120 ? 2 : 1, s);
-    if (merge) few_merge_kernel<D><<<static_cast<unsigned>(merge), kApThreads, 0, s>>>(a);
+    if (merge)
+      few_merge_kernel<D><<<static_cast<unsigned>(merge), kFewRows * D / 4, 0, s>>>(a);
   } else {
     const int64_t grid = std::min<int64_t>(units, kP4Units);
     prefill_kv4_kernel<D><<<static_cast<unsigned>(grid), kP4Threads, 0, s>>>(a);
