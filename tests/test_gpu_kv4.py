@@ -463,6 +463,32 @@ def test_replays_and_streams(wide):
     check_out(d0[0], d0[1], ref[idx], ref_lse[idx], size[idx], "decode")
 
 
+def test_calls_on_two_streams_at_once():
+    """Calls over one pool with workspaces of their own: as one after the other."""
+    c = Case(81, [900, 2000, 130, 64], 16, 4, 64, new=[40, 200, 1, 64], stale=0.1)
+    c.widen()
+    q, pool, meta, new = c.gpu()
+    last = torch.from_numpy(c.starts[1:].astype(np.int64) - 1).to("cuda")
+    lk.local_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, c.sm, **new)  # appends
+    w = torch.rand(c.table.shape, device="cuda")
+    pre = [lk.prepare_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, c.sm,
+                                             workspace=lk.Workspace()) for _ in range(2)]
+    dec = [lk.prepare_paged_attn_decode_kv4(q[last].contiguous(), pool, *meta, c.sm, weight_in=w,
+                                            workspace=lk.Workspace()) for _ in range(2)]
+    want = [t.clone() for t in pre[0]() + dec[0]()]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for s, p, d in zip(streams, pre, dec[::-1]):
+            with torch.cuda.stream(s):
+                p()
+                d()
+    torch.cuda.synchronize()
+    for p, d in zip(pre, dec):
+        for a, b in zip(p.outputs + d.outputs, want):
+            assert torch.equal(a, b)
+
+
 def test_binding_refusals():
     c = Case(61, [20], 4, 2, 64)
     q, pool, meta, new = c.gpu()
