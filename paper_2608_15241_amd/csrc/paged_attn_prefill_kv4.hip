@@ -251,13 +251,18 @@ __device__ void plan_kv4(const Prefill4Args& a) {
 // ---------------------------------------------------------------- append
 // The k-th block of new tokens: requests in order. Every lane returns the same; false
 // past the last.
-__device__ bool find_new_block(const Prefill4Args& a, int64_t k, int* b, int* j) {
+struct NewBlock {
+  int b, j;       // request, block of its table
+  int r0, n, L;   // the request's first token row and tokens, its context length
+};
+
+__device__ bool find_new_block(const Prefill4Args& a, int64_t k, NewBlock* f) {
   const int lane = threadIdx.x % kWave;
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    int n = 0, j0 = 0;
+    int n = 0, j0 = 0, r0 = 0, r1 = 0, L = 0;
     if (b0 + lane < a.B) {
-      const int r0 = a.q_indptr[b0 + lane], r1 = a.q_indptr[b0 + lane + 1];
-      const int L = a.ctx_lens[b0 + lane];
+      r0 = a.q_indptr[b0 + lane], r1 = a.q_indptr[b0 + lane + 1];
+      L = a.ctx_lens[b0 + lane];
       if (rows_ok4(r0, r1, a.T) && r1 > r0 && L > 0) {
         j0 = max(L - (r1 - r0), 0) / kBlockSize;
         n = min((L - 1) / kBlockSize + 1, a.max_blocks) - j0;
@@ -273,11 +278,15 @@ __device__ bool find_new_block(const Prefill4Args& a, int64_t k, int* b, int* j)
     const uint64_t past = __ballot(incl > k);
     if (past) {
       const int l = __builtin_ctzll(past);
-      *b = b0 + l;
-      *j = __shfl(j0, l) + static_cast<int>(k) - (__shfl(incl, l) - __shfl(n, l));
+      f->b = b0 + l;
+      f->r0 = __builtin_amdgcn_readlane(r0, l);
+      f->n = __builtin_amdgcn_readlane(r1, l) - f->r0;
+      f->L = __builtin_amdgcn_readlane(L, l);
+      f->j = __builtin_amdgcn_readlane(j0, l) + static_cast<int>(k) -
+             __builtin_amdgcn_readlane(incl - n, l);
       return true;
     }
-    k -= __shfl(incl, kWave - 1);
+    k -= __builtin_amdgcn_readlane(incl, kWave - 1);
   }
   return false;
 }
@@ -294,11 +303,11 @@ __global__ __launch_bounds__(kApThreads) void append_kv4_kernel(Prefill4Args a) 
                        threadIdx.x / kWave;
   const int lane = threadIdx.x % kWave, col = lane % 16, kgrp = lane / 16;
   const int g = static_cast<int>(unit % a.Hkv);
-  int b, j;
-  if (!find_new_block(a, unit / a.Hkv, &b, &j)) return;
-  const int p = a.block_table[static_cast<int64_t>(b) * a.max_blocks + j];
-  const int r0 = a.q_indptr[b], n = a.q_indptr[b + 1] - r0;
-  const int first = a.ctx_lens[b] - n;  // position of the chunk's first token
+  NewBlock f;
+  if (!find_new_block(a, unit / a.Hkv, &f)) return;
+  const int p = a.block_table[static_cast<int64_t>(f.b) * a.max_blocks + f.j];
+  const int r0 = f.r0, n = f.n, j = f.j;
+  const int first = f.L - n;  // position of the chunk's first token
   // Slot s of the block is token row s + off of the chunk where that is one of its n.
   const int off = j * kBlockSize - first;
   auto fresh = [&](int slot) { return slot + off >= 0 && slot + off < n; };
