@@ -265,7 +265,9 @@ def _on_device(on: Optional[int]):
 
 
 class Workspace:
-    """A grow-only device byte buffer reused across calls on one stream."""
+    """A grow-only device byte buffer that calls on one stream share. Calls that may run at
+    the same time (on several streams, or made by several threads) need one each: a call of a
+    few launches finds in its buffer what its own launches before wrote there."""
 
     def __init__(self, device=None):
         self.device = device
@@ -278,22 +280,17 @@ class Workspace:
         return self.buf
 
 
-_default_ws = {}
-
-
-def _ws_for(device) -> Workspace:
-    key = torch.device(device).index
-    if key not in _default_ws:
-        _default_ws[key] = Workspace(device)
-    return _default_ws[key]
-
-
 class Call:
     """One prepared C-ABI call: arguments marshalled once, replayed cheaply.
 
     The workspace size is queried once at preparation. Each call enqueues on
     the torch stream current at call time, so a sequence of prepared calls
     can be captured into a HIP graph (torch.cuda.graph) and replayed.
+
+    Given no workspace the call has one of its own (from torch's allocator), so
+    that it may run beside any other call; it has to be kept until its work has
+    run. What is shared is the caller's to order: a Workspace that several calls
+    were given, and one prepared call itself, which runs on one stream at a time.
     """
 
     def __init__(self, fn, args_before_ws, workspace: Optional[Workspace], device,
@@ -303,7 +300,7 @@ class Call:
         self.keep = tuple(t for t in keep if t is not None)
         n = ctypes.c_size_t(0)
         _check(fn(*args_before_ws, None, ctypes.byref(n), _stream()))
-        self.ws = (workspace or _ws_for(device)).get(n.value)
+        self.ws = (workspace or Workspace(device)).get(n.value)
         self.ws_bytes = ctypes.c_size_t(self.ws.numel())
         self.fn = fn
         self.args = tuple(args_before_ws) + (_ptr(self.ws), ctypes.byref(self.ws_bytes))
