@@ -95,7 +95,7 @@ constexpr size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(25
 
 // Logical blocks request b owns: ceil(L/16), at most the table's width.
 __device__ __forceinline__ int owned_blocks(int L, int max_blocks) {
-  return L <= 0 ? 0 : min((L + kBlockSize - 1) / kBlockSize, max_blocks);
+  return L <= 0 ? 0 : min((L - 1) / kBlockSize + 1, max_blocks);  // (L may be INT_MAX)
 }
 
 // Set bits of m below this lane.

@@ -30,7 +30,7 @@ __device__ __forceinline__ bool is_stale(const int32_t* __restrict__ table_row,
 }
 
 __device__ __forceinline__ int owned_blocks(int L, int max_blocks) {
-  return L <= 0 ? 0 : min((L + kBlockSize - 1) / kBlockSize, max_blocks);
+  return L <= 0 ? 0 : min((L - 1) / kBlockSize + 1, max_blocks);  // (L may be INT_MAX)
 }
 
 // Sums two ints over the workgroup; every thread gets the totals.
