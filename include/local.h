@@ -690,9 +690,9 @@ local_status_t local_paged_attn_prefill_kv4(
  *   block_version [num_blocks], req_version [B] int32
  *   table_out [B][max_blocks] int32, ctx_out [B] int32, weight_out
  *                [B][max_blocks] float32: each may be the input itself (in
- *                place), and must not overlap it otherwise
- *   evicted      [B][max_blocks] int32, n_evicted [B] int32; must not overlap an
- *                input
+ *                place)
+ *   evicted      [B][max_blocks] int32, n_evicted [B] int32
+ *  No output may overlap an input or another output otherwise (LOCAL_ERR_SHAPE).
  *  Sizes: B >= 0, max_blocks >= 1, num_blocks >= 1, sink_blocks >= 0,
  *  recent_blocks >= 1 (the last block, which the next token goes into, is always
  *  kept), block_size == 16. The result is exact and deterministic. No workspace.

@@ -169,3 +169,13 @@ constexpr float kLn2 = 0.6931471805599453f;
 // Host-side error reporting shared by the entry points (defined in capi.hip).
 local_status_t local_fail(local_status_t code, const char* fmt, ...);
 local_status_t local_check_launch(const char* what);
+
+namespace localk {
+
+// Whether na bytes from a and nb bytes from b share one.
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+}  // namespace localk

@@ -154,11 +154,6 @@ __global__ __launch_bounds__(kPoolWaves* kWave) void kv4_export_kernel(PoolArgs 
   }
 }
 
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
 local_status_t pool4_convert(bool import, PoolArgs a, int D, int block_size, void* stream) {
   const char* who = import ? "kv4_pool_import" : "kv4_pool_export";
   if (a.num_blocks < 0 || a.n < -1 || a.Hkv < 1)

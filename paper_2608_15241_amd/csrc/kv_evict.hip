@@ -204,6 +204,29 @@ extern "C" local_status_t local_kv_evict(const int32_t* block_table, int32_t B,
   if (!block_table || !ctx_lens || !block_weight || !keep_blocks || !block_version ||
       !req_version || !table_out || !ctx_out || !weight_out || !evicted || !n_evicted)
     return local_fail(LOCAL_ERR_NULL, "%s: NULL pointer argument", who);
+  // The first three outputs may be the inputs that they follow; a workgroup of one row
+  // would read what another has written anywhere else.
+  struct Array {
+    const void* p;
+    size_t bytes;
+  };
+  const size_t rows = static_cast<size_t>(B) * max_blocks * sizeof(int32_t);
+  const size_t each = static_cast<size_t>(B) * sizeof(int32_t);
+  const size_t tags = static_cast<size_t>(num_blocks) * sizeof(int32_t);
+  const Array in[] = {{block_table, rows}, {ctx_lens, each}, {block_weight, rows},
+                      {keep_blocks, each}, {req_version, each}, {block_version, tags}};
+  const Array o[] = {{table_out, rows}, {ctx_out, each}, {weight_out, rows},
+                     {evicted, rows}, {n_evicted, each}};
+  for (int i = 0; i < 5; ++i) {
+    bool bad = false;
+    for (int k = 0; k < 6; ++k)
+      bad |= !(i < 3 && k == i && o[i].p == in[k].p) &&
+             overlap(o[i].p, o[i].bytes, in[k].p, in[k].bytes);
+    for (int k = 0; k < i; ++k) bad |= overlap(o[i].p, o[i].bytes, o[k].p, o[k].bytes);
+    if (bad)
+      return local_fail(LOCAL_ERR_SHAPE, "%s: an output overlaps another array (only table_out, "
+                        "ctx_out and weight_out may be their inputs)", who);
+  }
   const EvictArgs a = {block_table, ctx_lens,   block_weight, keep_blocks, block_version,
                        req_version, table_out,  ctx_out,      weight_out,  evicted,
                        n_evicted,   num_blocks, max_blocks,   sink_blocks, recent_blocks};
