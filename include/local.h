@@ -419,7 +419,7 @@ local_status_t local_paged_attn_decode_noalloc(
  *   weight_in     [B][max_blocks] float32, or NULL (zeros)
  *   weight_decay  in [0, 1]
  *   weight_out    [B][max_blocks] float32; may be weight_in itself (in place),
- *                 must not overlap it otherwise
+ *                 must not overlap it otherwise (LOCAL_ERR_SHAPE)
  *  All other arguments, the results in out/lse and the appended slots: as
  *  local_paged_attn_decode. Weights are float32 sums in a fixed order.
  *  Errors as local_paged_attn_decode; LOCAL_ERR_NULL for a NULL weight_out with

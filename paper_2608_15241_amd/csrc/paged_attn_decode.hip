@@ -744,6 +744,8 @@ extern "C" local_status_t local_paged_attn_decode_weighted(
   if (B == 0) return LOCAL_OK;
   if ((st = decode_pointers_ok(a, who)) != LOCAL_OK) return st;
   if (!weight_out) return local_fail(LOCAL_ERR_NULL, "%s: weight_out is NULL", who);
+  if ((st = decode_weights_apart(weight_in, weight_out, B, max_blocks, who)) != LOCAL_OK)
+    return st;
   a.blk_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(part.bytes));
   a.w_in = weight_in;
   a.w_out = weight_out;

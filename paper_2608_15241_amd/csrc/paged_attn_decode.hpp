@@ -438,6 +438,15 @@ inline local_status_t decode_weights_ok(int Hq, float decay, const char* who) {
   return LOCAL_OK;
 }
 
+// weight_out is weight_in itself (a thread reads and writes the same element) or apart.
+inline local_status_t decode_weights_apart(const float* in, const float* out, int B,
+                                           int max_blocks, const char* who) {
+  const size_t bytes = static_cast<size_t>(B) * max_blocks * sizeof(float);
+  if (in && in != out && overlap(in, bytes, out, bytes))
+    return local_fail(LOCAL_ERR_SHAPE, "%s: weight_out overlaps weight_in in part", who);
+  return LOCAL_OK;
+}
+
 inline size_t block_lse_bytes(int B, int Hq, int max_blocks) {
   return align256(static_cast<size_t>(B > 0 ? B : 1) * Hq * max_blocks * sizeof(float));
 }

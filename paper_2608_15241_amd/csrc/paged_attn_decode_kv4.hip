@@ -368,6 +368,8 @@ extern "C" local_status_t local_paged_attn_decode_kv4(
       !aligned16(v_new) || !aligned16(ws))
     return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: q, k_new, v_new, kv4, out and ws must start "
                       "on 16 bytes", who);
+  if ((st = decode_weights_apart(weight_in, weight_out, B, max_blocks, who)) != LOCAL_OK)
+    return st;
   a.part_o = static_cast<float*>(ws);
   a.part_ml = a.part_o + part.elems * D;
   a.blk_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(part.bytes));

@@ -46,3 +46,17 @@ def test_evict_outputs(lib, out, other):
         if shift == 0 and out == other + "_out":
             continue  # in place: allowed
         _refused(lib, _evict(lib, **{out: at + shift}), (out, other, shift))
+
+
+@pytest.mark.parametrize("shift", [4, -4, ROWS - 4, 4 - ROWS])
+@pytest.mark.parametrize("name", ["local_paged_attn_decode_weighted",
+                                  "local_paged_attn_decode_kv4"])
+def test_weights_in_part(lib, name, shift):
+    a = lambda i: ctypes.c_void_p(0x100000 * i)  # noqa: E731
+    pools = [a(4)] if name.endswith("kv4") else [a(4), a(5)]
+    n = ctypes.c_size_t(1 << 40)
+    status = getattr(lib, name)(a(1), B, 8, 4, 64, a(2), a(3), *pools, NB, 16, a(6), MB, a(7),
+                                a(8), a(9), 0.1, a(10), a(11), a(12), 1.0,
+                                ctypes.c_void_p(0x100000 * 12 + shift), a(13), ctypes.byref(n),
+                                None)
+    _refused(lib, status, (name, shift))
