@@ -610,7 +610,8 @@ local_status_t local_kv4_pool_export(
  *   kv4          4-bit pool of num_blocks blocks; written only at the appended
  *                slots
  *   weight_in, weight_decay, weight_out   as local_paged_attn_decode_weighted;
- *                weight_out NULL: no weights (then weight_in must be NULL)
+ *                weight_out NULL: no weights (then weight_in must be NULL,
+ *                weight_decay is ignored and Hq is not limited)
  *   other arguments as in decode.
  *
  *  A group that stands for NaN makes the outputs NaN that it enters (a stale

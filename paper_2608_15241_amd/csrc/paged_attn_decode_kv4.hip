@@ -330,7 +330,7 @@ extern "C" local_status_t local_paged_attn_decode_kv4(
     return local_fail(LOCAL_ERR_NULL, "%s: k_new and v_new must both be set", who);
   if (weight_in && !weight_out)
     return local_fail(LOCAL_ERR_NULL, "%s: weight_in without weight_out", who);
-  local_status_t st = decode_weights_ok(Hq, weight_decay, who);
+  local_status_t st = weight_out ? decode_weights_ok(Hq, weight_decay, who) : LOCAL_OK;
   if (st != LOCAL_OK) return st;
   DecodeArgs a{};
   a.q = q;
