@@ -648,7 +648,11 @@ local_status_t local_paged_attn_decode_kv4(
  *  whose values are not finite does not reach it.
  *  Sizes and errors as local_paged_attn_prefill, T * Hq / Hkv below 2^30; q, k_new,
  *  v_new, kv4, out and ws must start on 16 bytes (LOCAL_ERR_UNSUPPORTED
- *  otherwise). Workspace: the size asked for.
+ *  otherwise).
+ *  Workspace: the size asked for, which is not monotone in T and B (calls of few and
+ *  of many rows a request go different ways). A workspace of
+ *    2^18 * (D + 2) * 4 + 64 * (T * Hq / Hkv / 128 + B) + 49408 bytes
+ *  serves every call of at most T rows and B requests, whatever its table's width.
  */
 local_status_t local_paged_attn_prefill_kv4(
     const uint16_t* q, const int32_t* q_indptr, int32_t B, int64_t T,

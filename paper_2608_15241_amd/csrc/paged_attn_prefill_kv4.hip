@@ -927,7 +927,7 @@ __global__ __launch_bounds__(kApThreads) void merge_kv4_kernel(Prefill4Args a) {
 // Requests that bring few rows each (a token or a few behind a long context) leave most
 // of a 128-row tile empty, and their time is that of reading the cache: as in decode, one
 // wave (or two or four, whose results meet in LDS) takes 16 rows of a request and KV head
-// over a partition of up to 64 blocks, in its registers (kv4_attn.hpp). A request with
+// over a partition of the blocks, in its registers (kv4_attn.hpp). A request with
 // more rows takes several such units, which read the same blocks.
 constexpr int kFewRows = 16;
 
@@ -985,7 +985,7 @@ __device__ __forceinline__ int64_t few_row(const Prefill4Args& a, const FewTile&
 }
 
 template <int D, int W>
-__global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
+__global__ __launch_bounds__(kWave* W, W == 1 ? 4 : 3) void few_kv4_kernel(Prefill4Args a) {
   using L4 = Kv4<D>;
   constexpr int DEPTH = 2;  // pairs of blocks in registers
   const int lane = threadIdx.x % kWave, col = lane % 16, kgrp = lane / 16;
@@ -1001,17 +1001,19 @@ __global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
   const int jend = t.blocks - part * a.pb, j0 = max(0, jend - a.pb);
   const int32_t* table = a.block_table + static_cast<int64_t>(t.b) * a.max_blocks;
   const int rv = a.req_version[t.b];
-  int my_phys = 0;
-  bool ok = false;
-  if (lane < a.pb && j0 + lane < jend) {
-    my_phys = table[j0 + lane];
-    ok = my_phys >= 0 && my_phys < a.num_blocks && a.block_version[my_phys] == rv;
-    if (!ok) my_phys = 0;  // an id outside the pool is never dereferenced
-  }
-  const uint64_t part_valid = __ballot(ok);
-  uint64_t valid = part_valid;
-  if (W > 1)
-    valid = __ballot(ok && __popcll(part_valid & ((1ull << lane) - 1ull)) % W == wave);
+  // A group of 64 blocks from jg on, a lane each: this wave's share of the valid ones.
+  int jg = j0, my_phys = 0;
+  uint64_t valid = 0ull;
+  auto take = [&](int id) {
+    const bool ok =
+        jg + lane < jend && id >= 0 && id < a.num_blocks && a.block_version[id] == rv;
+    my_phys = ok ? id : 0;  // an id outside the pool is never dereferenced
+    const uint64_t all = __ballot(ok);
+    valid = all;
+    if (W > 1) valid = __ballot(ok && __popcll(all & ((1ull << lane) - 1ull)) % W == wave);
+  };
+  auto read_id = [&](int j) { return j + lane < jend ? table[j + lane] : -1; };
+  take(read_id(jg));
 
   Attn4<D> at;
   const bool in = col < t.rows;
@@ -1054,7 +1056,7 @@ __global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
     bool hit = false;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int i = e ? i1 : i0, j = j0 + i;
+      const int i = e ? i1 : i0, j = jg + i;
       // a block that some row sees in part, or none
       const bool tail = i < 0 || j * kBlockSize + kBlockSize - 1 > t.first;
       const int seen = i < 0 ? 0 : min(max(pos - j * kBlockSize + 1, 0), kBlockSize);
@@ -1088,19 +1090,24 @@ __global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
       load_block4<D>(R[d], e, a.kv4, static_cast<int64_t>(p) * a.Hkv + g, i >= 0);
     }
   };
+  for (;;) {
 #pragma unroll
-  for (int d = 0; d < DEPTH - 1; ++d) fill(d);
-  bool done = false;
-  while (!done) {
+    for (int d = 0; d < DEPTH - 1; ++d) fill(d);
+    bool done = false;
+    while (!done) {
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      fill((d + DEPTH - 1) % DEPTH);
-      if (i0[d] < 0) {
-        done = true;
-        break;
+      for (int d = 0; d < DEPTH; ++d) {
+        fill((d + DEPTH - 1) % DEPTH);
+        if (i0[d] < 0) {
+          done = true;
+          break;
+        }
+        compute(R[d], i0[d], i1[d]);
       }
-      compute(R[d], i0[d], i1[d]);
     }
+    jg += kWave;
+    if (jg >= jend) break;
+    take(read_id(jg));
   }
 
   extern __shared__ __attribute__((aligned(16))) float mg[];
@@ -1194,6 +1201,23 @@ bool few_rows(int64_t all_rows, int B, int Hkv, int max_blocks) {
          all_rows / kFewRows + B <= kFewWork / max_blocks / Hkv;
 }
 
+// Blocks of a partition of such a call: as in decode up to kFewMost units (tile, KV head,
+// partition of a table's row), of which each may leave 16 rows of partial results, 136 MB
+// in all at D = 128; beyond, as many times 64 blocks as leave no more. (Without a bound 128
+// requests of 32 tokens with 32 heads and a 1024-block table ask for 1.1 GB.) Measured in us
+// without / with at most 16384 / 8192 / 4096 units: 128 requests of 4 tokens behind up to
+// 16000, 32/8 heads, 300 / 294 / 308 / 326; 64 of 8 behind up to 8000 142 / 147 / 144 / 154;
+// 32 of 32 behind up to 4000, 32 heads each, 165 / 154 / 150 / 124; 200 single tokens
+// behind up to 16000 373 / 374 / 415 / 386.
+constexpr int64_t kFewMost = 16384;
+
+int few_part_blocks(int max_blocks, int64_t heads) {  // heads: tiles * Hkv
+  const int pb = part_blocks(max_blocks, heads);
+  if (heads * parts_of_table(max_blocks, pb) <= kFewMost) return pb;
+  const int parts = static_cast<int>(std::max<int64_t>(1, kFewMost / heads));
+  return (max_blocks + kWave * parts - 1) / (kWave * parts) * kWave;
+}
+
 // Key ranges that a tile of a call may be split into: as many as give every compute unit
 // a workgroup where there are few tiles, counted from the sizes that the host knows.
 int ranges_of_call(int64_t tiles, int Hkv, int max_blocks) {
@@ -1202,6 +1226,16 @@ int ranges_of_call(int64_t tiles, int Hkv, int max_blocks) {
   const int least = least_range(tiles * Hkv);
   const int64_t most = std::max(1, (max_blocks + least / 2) / least);
   return static_cast<int>(std::min<int64_t>({want, most, kP4MaxRanges}));
+}
+
+// Tiles of a call; sets a's partitions (few rows) or else pb = 0, and its ranges.
+int64_t tiles_of_call(Prefill4Args& a, int64_t all_rows, int B, int Hkv, int max_blocks) {
+  const bool few = few_rows(all_rows, B, Hkv, max_blocks);
+  // (B tiles more than the rows fill: each request's last one)
+  const int64_t tiles = all_rows / (few ? kFewRows : kP4Rows) + B;
+  a.pb = few ? few_part_blocks(max_blocks, tiles * Hkv) : 0;
+  a.ranges = few ? parts_of_table(max_blocks, a.pb) : ranges_of_call(tiles, Hkv, max_blocks);
+  return tiles;
 }
 
 }  // namespace
@@ -1230,19 +1264,11 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   if ((k_new == nullptr) != (v_new == nullptr))
     return local_fail(LOCAL_ERR_NULL, "%s: k_new and v_new must both be set", who);
   Prefill4Args a{};
-  const int64_t all_rows = T * (Hq / Hkv);
-  const bool few = few_rows(all_rows, B, Hkv, max_blocks);
-  // (B tiles more than the rows fill: each request's last one)
-  const int64_t tiles = all_rows / (few ? kFewRows : kP4Rows) + B;
+  const int64_t tiles = tiles_of_call(a, T * (Hq / Hkv), B, Hkv, max_blocks);
   if (tiles * kP4MaxRanges >= (1LL << 31))
     return local_fail(LOCAL_ERR_UNSUPPORTED, "%s: T=%lld B=%d", who, (long long)T, B);
   a.max_tiles = static_cast<int>(tiles);
-  if (few) {
-    a.pb = part_blocks(max_blocks, tiles * Hkv);
-    a.ranges = parts_of_table(max_blocks, a.pb);
-  } else {
-    a.ranges = ranges_of_call(tiles, Hkv, max_blocks);
-  }
+  const bool few = a.pb != 0;
   const size_t rows = static_cast<size_t>(T) * Hq * (a.ranges > 1 ? a.ranges : 0);
   const size_t tiles_at = few ? 0 : sizeof(Unit4) * tiles * a.ranges;
   const size_t part_at = few ? 0 : align256(tiles_at + sizeof(int4) * tiles);
@@ -1291,4 +1317,14 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   a.q_and = scale.q_and;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return D == 64 ? launch_prefill_kv4<64>(a, s) : launch_prefill_kv4<128>(a, s);
+}
+
+// What a call's size selects: 16 rows at a time, the blocks of a partition; 128 rows, minus
+// the most key ranges of a tile (for the tests, which name the form that they mean; not in
+// local.h).
+extern "C" int32_t localk_prefill_kv4_form(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
+                                           int32_t max_blocks) {
+  Prefill4Args a{};
+  tiles_of_call(a, T * (Hq / Hkv), B, Hkv, max_blocks);
+  return a.pb ? a.pb : -a.ranges;
 }
