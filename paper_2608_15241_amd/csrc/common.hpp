@@ -109,13 +109,17 @@ __device__ __forceinline__ u32x2 buf_load8_stream(__amdgpu_buffer_rsrc_t r, uint
 }
 
 // ---------------------------------------------------------------- lanes
-// max(a, b) in one instruction: fmaxf of values the compiler cannot prove
-// canonical (a lane swap's result, say) adds a NaN-quieting maximum per
-// operand. The operands here are never NaN.
+// Maxima in one instruction each, NaN if an operand is (fmaxf of values that the compiler
+// cannot prove canonical, a lane swap's result, say, adds a NaN-quieting maximum per
+// operand). Not as inline assembly: the compiler puts the waits that the result of a matrix
+// product or of an exponential needs before its own instructions only, and a maximum that
+// reads too early reads an old register.
 __device__ __forceinline__ float max2f(float a, float b) {
-  float r;
-  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-  return r;
+  return __builtin_elementwise_maximum(a, b);
+}
+
+__device__ __forceinline__ float max3f(float a, float b, float c) {
+  return max2f(max2f(a, b), c);
 }
 
 // Maximum of v over lanes l and l ^ 16 (l ^ 32), by the gfx950 lane swaps of

@@ -180,13 +180,6 @@ __device__ __forceinline__ uint32_t round_v(u32x4 v, uint32_t& code) {
   return s;
 }
 
-// max(a, b, c) in one instruction, NaN if one is (fmaxf would first quiet each operand).
-// Not as inline assembly: the compiler puts the waits that a product's result needs before
-// its own instructions only, and a maximum read too early is an old register's.
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
-}
-
 // Softmax scale in log2 units, kept positive so that the largest raw score is the
 // largest score: a negative scale flips q's signs, a zero one (every visible key then
 // weighs the same) clears q.

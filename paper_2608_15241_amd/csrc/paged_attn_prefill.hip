@@ -47,12 +47,6 @@ constexpr float kMaskedScore = -3.0e38f;   // score of a key a row may not see
 constexpr float kPaLazy = 8.0f;            // log2 of the largest weight before a rescale
 constexpr float kPaLazyWeight = 256.0f;    // 2^kPaLazy
 
-// max(a, b, c) in one instruction (fmaxf chains add NaN-quieting maxima)
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
 // Tiles whose causal range spans more than kPaSplitBlocks blocks (less in calls
 // of few tiles: few_ranges below) are split into up to kPaMaxSplit key ranges of
 // equal length, each its own workgroup; a merge launch combines their partial
