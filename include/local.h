@@ -616,6 +616,9 @@ local_status_t local_kv4_pool_export(
  *
  *  A group that stands for NaN makes the outputs NaN that it enters (a stale
  *  block's, or a slot past ctx_lens[b], enters none).
+ *  The softmax weights are rounded to bf16 for their products with V (2^-8 of each
+ *  at most) and each output is divided by the sum of the rounded ones; lse and the
+ *  block weights come from the unrounded ones.
  *  Sizes and errors as local_paged_attn_decode; q, k_new, v_new, kv4, out and ws
  *  must start on 16 bytes (LOCAL_ERR_UNSUPPORTED otherwise). Workspace: the size
  *  asked for.
@@ -646,6 +649,7 @@ local_status_t local_paged_attn_decode_kv4(
  *
  *  A row's result depends only on the keys it sees: a later token of its chunk
  *  whose values are not finite does not reach it.
+ *  Softmax weights are rounded as in decode.
  *  Sizes and errors as local_paged_attn_prefill, T * Hq / Hkv below 2^30; q, k_new,
  *  v_new, kv4, out and ws must start on 16 bytes (LOCAL_ERR_UNSUPPORTED
  *  otherwise).

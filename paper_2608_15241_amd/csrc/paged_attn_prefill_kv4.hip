@@ -22,7 +22,7 @@
 //    into registers while the next is unpacked and this one computed; one barrier.
 //  * S^T = K Q^T, O^T += V^T P^T on v_mfma_f32_16x16x32_bf16, as in decode, and as
 //    there the running maximum rises only when a weight would pass 2^8, and the weights
-//    are rounded to bf16 for the product but not for their sum. 4 x 512 tokens on 0 to
+//    are rounded to bf16 for the product and summed both ways. 4 x 512 tokens on 0 to
 //    2048, 32 heads of 128: 78 us, the steps at 860 TFLOP/s (977 behind 8192).
 //  * An infinity or a NaN in V (scale byte 255) must reach the rows that see its token
 //    and no other, which 0 * NaN in a product would not do: its values enter the
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
   read_q(e, g);
 
   f32x4 acc[RT][VT];
-  float m_run[RT], l_run[RT], rise[RT];
+  float m_run[RT], rise[RT], l_run[RT], w_run[RT];  // as in Attn4
   const float inv_scale = 1.f / a.scale_log2;
   // Positions of the wave's first and last row: bounds of what it may see.
   bool wave_full = false;
@@ -613,6 +613,7 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
         const float m_new = fmaxf(m_run[r], max_xor32(max_xor16(mx)) * a.scale_log2);
         const float alpha = fast_exp2(m_run[r] - m_new);
         l_run[r] *= alpha;
+        w_run[r] *= alpha;
         m_run[r] = m_new;
         rise[r] = (m_new + kLazy4) * inv_scale;
 #pragma unroll
@@ -630,6 +631,10 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
         pf[r][e / 2][2 * (e % 2) + 1] = pack_bf16x2(p[2], p[3]);
       }
       l_run[r] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+      for (int e = 0; e < kP4Step / 2; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w_run[r] = add_pair(pf[r][e][k], w_run[r]);
     }
 #pragma unroll
     for (int q = 0; q < kGroups; ++q) {
@@ -782,7 +787,7 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       m_run[r] = kNegBig4;
-      l_run[r] = 0.f;
+      l_run[r] = w_run[r] = 0.f;
       rise[r] = (kNegBig4 + kLazy4) * inv_scale;
 #pragma unroll
       for (int t = 0; t < VT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -841,6 +846,9 @@ __global__ __launch_bounds__(kP4Threads, 2) void prefill_kv4_kernel(Prefill4Args
     for (int r = 0; r < RT; ++r) {
       l_run[r] += __shfl_xor(l_run[r], 16);
       l_run[r] += __shfl_xor(l_run[r], 32);
+      const float fit = rounded_fit(l_run[r], sum_kgroups(w_run[r]));
+#pragma unroll
+      for (int t = 0; t < VT; ++t) acc[r][t] *= fit;
     }
     if (half == 0)
       hand_over(acc[1], m_run[1], l_run[1], 1);
@@ -985,7 +993,7 @@ __device__ __forceinline__ int64_t few_row(const Prefill4Args& a, const FewTile&
 }
 
 template <int D, int W>
-__global__ __launch_bounds__(kWave* W, W == 1 ? 4 : 3) void few_kv4_kernel(Prefill4Args a) {
+__global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
   using L4 = Kv4<D>;
   constexpr int DEPTH = 2;  // pairs of blocks in registers
   const int lane = threadIdx.x % kWave, col = lane % 16, kgrp = lane / 16;

@@ -62,9 +62,9 @@ def test_long_partitions(i):
     import paper_2608_15241_amd as lk
     from tests.gpu_helpers import dev, say
     from tests.kv4_helpers import check_out
-    from tests.test_gpu_kv4 import Case
+    from tests.kv4_cases import quick_case
     prefix, chunk, hq, hkv, D, width, _ = LONG[i]
-    c = Case(300 + i, np.array(prefix) + np.array(chunk), hq, hkv, D, new=chunk, stale=0.3)
+    c = quick_case(300 + i, np.array(prefix) + np.array(chunk), hq, hkv, D, new=chunk, stale=0.3)
     c.tags[c.table[0, 60:200][c.table[0, 60:200] >= 0] % c.num] -= 1  # a group wholly stale
     c.widen()
     assert c.table.shape[1] == width
