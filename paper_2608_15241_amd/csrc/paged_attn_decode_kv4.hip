@@ -277,6 +277,15 @@ int kv4_waves(const DecodeArgs& a, int B) {
   return units < (a.n_parts > 1 ? 5120 : 2048) ? 2 : 1;
 }
 
+// Whether units are dispatched longest first. Units that are about all resident at once
+// need no order, and finding it takes a call of 4 requests 1 us of 6.7; 128 short requests,
+// 4096 waves, 15.4 us with and 14.1 without, 16 of up to 4000 tokens, 4352 waves, 18.0 with
+// and 18.7 without.
+bool kv4_ranked(const DecodeArgs& a, int B) {
+  const int64_t wgs = static_cast<int64_t>(a.Hkv) * B * (a.n_parts + 1);
+  return B <= kRankChunks * kWave && wgs * kv4_waves(a, B) > 4096;
+}
+
 template <int D>
 local_status_t launch_decode_kv4(const DecodeArgs& a, int B, hipStream_t s) {
   const int64_t wgs = static_cast<int64_t>(a.Hkv) * B * (a.n_parts + 1);
@@ -285,10 +294,7 @@ local_status_t launch_decode_kv4(const DecodeArgs& a, int B, hipStream_t s) {
     return local_fail(LOCAL_ERR_UNSUPPORTED, "paged_attn_decode_kv4: grid of %lld workgroups",
                       (long long)std::max(wgs, merge));
   const int W = kv4_waves(a, B);
-  // (units that are about all resident at once need no order, and finding it takes a call
-  // of 4 requests 1 us of 6.7; 128 short requests, 4096 waves, 15.4 us with and 14.1
-  // without, 16 of up to 4000 tokens, 4352 waves, 18.0 with and 18.7 without)
-  const bool ranked = B <= kRankChunks * kWave && wgs * W > 4096;
+  const bool ranked = kv4_ranked(a, B);
   const unsigned grid =
       static_cast<unsigned>(a.Hkv) * B * static_cast<unsigned>(a.n_parts + (ranked ? 1 : 0));
   if (ranked)
@@ -378,4 +384,17 @@ extern "C" local_status_t local_paged_attn_decode_kv4(
   a.w_decay = weight_decay;
   hipStream_t s = static_cast<hipStream_t>(stream);
   return D == 64 ? launch_decode_kv4<64>(a, B, s) : launch_decode_kv4<128>(a, B, s);
+}
+
+// The partition length, the waves and the dispatch order that a call's size selects, as
+// blocks + 256 x waves + 4096 if longest first (for the tests, which name the form that they
+// mean; not in local.h).
+extern "C" int32_t localk_decode_kv4_form(int32_t B, int32_t Hq, int32_t Hkv,
+                                          int32_t max_blocks) {
+  DecodeArgs a{};
+  a.Hkv = Hkv;
+  a.group = Hq / Hkv;
+  a.max_blocks = max_blocks;
+  decode_parts(a, B, 128, true);
+  return a.pb + 256 * kv4_waves(a, B) + (kv4_ranked(a, B) ? 4096 : 0);
 }

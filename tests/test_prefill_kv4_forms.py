@@ -59,9 +59,7 @@ def test_long_partitions_are_the_named_ones(i):
 @pytest.mark.gpu
 @pytest.mark.parametrize("i", range(len(LONG)))
 def test_long_partitions(i):
-    import paper_2608_15241_amd as lk
-    from tests.gpu_helpers import dev, say
-    from tests.kv4_helpers import check_out
+    from tests.gpu_helpers import say
     from tests.kv4_cases import quick_case
     prefix, chunk, hq, hkv, D, width, _ = LONG[i]
     c = quick_case(300 + i, np.array(prefix) + np.array(chunk), hq, hkv, D, new=chunk, stale=0.3)
@@ -69,9 +67,98 @@ def test_long_partitions(i):
     c.widen()
     assert c.table.shape[1] == width
     say("long partitions", i, prefix[:3], chunk[:3], hq, hkv, D)
+    _run(c, range(len(chunk)))
+
+
+def _check(c, b, out, lse, want, sm):
+    """The rows of one request."""
+    from oracle import kv4
+    from tests.kv4_cases import check_counts
+    from tests.kv4_helpers import check_out
+    from tests.pool_helpers import bits_to_f64
+    rows = slice(c.starts[b], c.starts[b + 1])
+    if rows.start == rows.stop:
+        return
+    K, V = want
+    ref, ref_lse, size, _ = kv4.attention(
+        bits_to_f64(c.q[rows]), [0, c.new[b]], c.ctx[b:b + 1], c.table[b:b + 1], c.tags,
+        c.version[b:b + 1], K, V, sm)
+    if sm:
+        check_out(out[rows], lse[rows], ref, ref_lse, size, "request %d" % b)
+    else:
+        check_counts(out[rows], lse[rows], ref, ref_lse, "request %d at 0" % b)
+
+
+def _run(c, requests):
+    import paper_2608_15241_amd as lk
+    from oracle import kv4
+    from tests.gpu_helpers import dev
     q, pool, meta, new = c.gpu()
-    want = c.appended()
-    ref, ref_lse, size, _ = c.ref(want)
-    out, lse = lk.local_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, c.sm, **new)
-    check_out(out, lse, ref, ref_lse, size, "out")
-    assert np.array_equal(pool.cpu().numpy(), want)
+    tiles = c.appended()
+    want = kv4.unpack(tiles)
+    for sm in (c.sm, 0.0):
+        out, lse = lk.local_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, sm, **new)
+        for b in requests:
+            _check(c, b, out, lse, want, sm)
+    assert np.array_equal(pool.cpu().numpy(), tiles)
+
+
+# A tile of 128 rows over more keys than a window lists (512 blocks): windows whose edge lies
+# among stale blocks, one wholly stale, a last one of a single block.
+WINDOWS = [(17600, 32, 16, 64), (8250, 32, 16, 128), (16 * 1025 - 40, 64, 8, 64)]
+
+
+@pytest.mark.parametrize("prefix,B,hkv,D", WINDOWS)
+def test_windows_are_of_one_range(prefix, B, hkv, D):
+    assert _form(40 * B, B, hkv, hkv, (prefix + 55) // 16) == -1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prefix,B,hkv,D", WINDOWS)
+def test_several_windows(prefix, B, hkv, D):
+    from tests.gpu_helpers import say
+    from tests.kv4_cases import quick_case
+    chunk = np.full(B, 40)
+    before = np.arange(B) * 7 % 50
+    before[0] = prefix
+    c = quick_case(B + D, before + chunk, hkv, hkv, D, new=chunk, stale=0.2)
+    nb = (prefix + 55) // 16
+    gone = np.r_[505:520, 520:1020 if nb > 1024 else 513]
+    gone = gone[gone < nb - 4]
+    c.table[0, gone] = np.where(gone % 3 == 0, -1, c.table[0, gone])
+    inside = c.table[0, gone][(c.table[0, gone] >= 0) & (c.table[0, gone] < c.num)]
+    c.tags[inside] = c.version[0] + 1
+    say("windows", prefix, B, hkv, D)
+    _run(c, [0, 1, B - 1])
+
+
+# More requests than the planner scans at once (256), more tiles than it keeps in LDS (1024),
+# both, and tiles that spill while every request's sizes are at hand.
+PLANS = [(300, 9, 13, 60, 32, 8, 64), (1100, 2, 5, 130, 16, 1, 64), (200, 40, 60, 60, 16, 1, 64)]
+
+
+@pytest.mark.parametrize("B,lo,hi,prefix,hq,hkv,D", PLANS)
+def test_plans_are_of_128_rows(B, lo, hi, prefix, hq, hkv, D):
+    chunk = _chunks(B, lo, hi)
+    assert _form(chunk.sum(), B, hq, hkv, (prefix + hi + 15) // 16) < 0
+    tiles = sum(-(-n * (hq // hkv) // 128) for n in chunk)
+    assert B > 256 or tiles > 1024
+
+
+def _chunks(B, lo, hi):
+    return np.random.default_rng(B).integers(lo, hi, B)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,lo,hi,prefix,hq,hkv,D", PLANS)
+def test_large_plans(B, lo, hi, prefix, hq, hkv, D):
+    from tests.gpu_helpers import say
+    from tests.kv4_cases import quick_case
+    chunk = _chunks(B, lo, hi)
+    before = np.random.default_rng(B + 1).integers(0, prefix, B)
+    c = quick_case(B, before + chunk, hq, hkv, D, new=chunk, stale=0.1,
+                   width=(prefix + hi + 15) // 16)
+    say("plans", B, lo, hi, prefix, hq, hkv, D)
+    some = np.unique(np.r_[0, 63, 64, 127, 128, 255, 256, 257, 511, 512, B - 2, B - 1,
+                           np.random.default_rng(2).integers(0, B, 25)])
+    _run(c, some[some < B])
