@@ -690,8 +690,13 @@ local_status_t local_paged_attn_prefill_kv4(
  *    evicted[b, 0..nb_b-n_b) ids of the evicted blocks in ascending j, then -1
  *    n_evicted[b]            nb_b - n_b
  *  No KV is moved: the pool's blocks stay as they are, and the caller returns
- *  the evicted ids to its allocator (a block that another request's table
- *  holds too is the caller's to count).
+ *  the evicted ids to its allocator. A block that another request's table
+ *  holds too is the caller's to count, and a stale entry's id is listed as it
+ *  stood in the table: it may lie outside the pool, or name a block that
+ *  belongs to another request by now.
+ *  A row that lost blocks no longer holds its token path: it must not be
+ *  recorded in the prefix table (local_kvm_insert), which would take block j
+ *  for tokens 16 j .. 16 j + 15.
  *
  *   block_table  [B][max_blocks] int32;  ctx_lens [B] int32 in [0, 16*max_blocks]
  *   block_weight [B][max_blocks] float32

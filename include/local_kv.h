@@ -182,7 +182,8 @@ local_status_t local_kvm_lookup(local_kvm_t* m, int32_t ns, int32_t adapter, int
  * matched them), so that an adapter state's records always form a prefix of
  * each path. recorded[i] = 1 when the block was recorded, 0 when the node
  * already had a record for this adapter state (that record stays; the caller
- * releases blocks[i]). recorded may be NULL. */
+ * releases blocks[i]). recorded may be NULL. (A table that local_kv_evict has
+ * closed up no longer holds its path's blocks in place: it is not inserted.) */
 local_status_t local_kvm_insert(local_kvm_t* m, int32_t ns, int32_t adapter, int32_t version,
                                 const int32_t* tokens, int64_t n_tokens, int32_t first,
                                 const int32_t* blocks, int32_t n_blocks, int32_t* recorded);

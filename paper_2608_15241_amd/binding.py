@@ -290,7 +290,8 @@ class Call:
     Given no workspace the call has one of its own (from torch's allocator), so
     that it may run beside any other call; it has to be kept until its work has
     run. What is shared is the caller's to order: a Workspace that several calls
-    were given, and one prepared call itself, which runs on one stream at a time.
+    were given, and one prepared call itself, which one thread at a time makes, on one
+    stream.
     """
 
     def __init__(self, fn, args_before_ws, workspace: Optional[Workspace], device,

@@ -15,7 +15,7 @@
 //  * Blocks are taken in pairs (kv4_attn.hpp).
 //  * Partitions, dispatch order, waves per partition and merge: as for bf16.
 // 128 contexts of 1024 to 16384 tokens, 8 KV heads of 128, weights of the blocks too:
-// 214 us, 5.1 TB/s (the loads alone take 95% of it).
+// 218 us, 5.0 TB/s (the loads alone take 95% of it).
 #include "kv4_attn.hpp"
 #include "paged_attn_decode.hpp"
 

@@ -785,8 +785,8 @@ __global__ __launch_bounds__(kPaThreads, 2) void prefill_attn_kernel(PrefillArgs
       // p = 2^(scale (s - m)) with the running maximum m, one fused
       // multiply-add and one exponent each. Lazy rescale: m moves only when
       // a column's maximum exceeds it by more than 2^kPaLazy in weight, i.e.
-      // when some p exceeds 2^kPaLazy (weights up to that stay exact in
-      // float32 and bf16 alike, so the result is the same softmax); then m,
+      // when some p exceeds 2^kPaLazy (float32 and bf16 hold weights up to
+      // that as well as below 1, so the result is the same softmax); then m,
       // the sums and the weights are redone, which is rare after the first
       // step. Testing the weights instead of the scores leaves the common
       // step without the cross-lane maxima.

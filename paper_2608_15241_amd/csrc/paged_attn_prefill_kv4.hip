@@ -23,7 +23,7 @@
 //  * S^T = K Q^T, O^T += V^T P^T on v_mfma_f32_16x16x32_bf16, as in decode, and as
 //    there the running maximum rises only when a weight would pass 2^8, and the weights
 //    are rounded to bf16 for the product and summed both ways. 4 x 512 tokens on 0 to
-//    2048, 32 heads of 128: 78 us, the steps at 860 TFLOP/s (977 behind 8192).
+//    2048, 32 heads of 128: 78 us, the steps at about 850 TFLOP/s.
 //  * An infinity or a NaN in V (scale byte 255) must reach the rows that see its token
 //    and no other, which 0 * NaN in a product would not do: its values enter the
 //    product as zeros, and a mask of such tokens then puts NaN into those rows.
