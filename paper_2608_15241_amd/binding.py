@@ -288,10 +288,9 @@ class Call:
     can be captured into a HIP graph (torch.cuda.graph) and replayed.
 
     Given no workspace the call has one of its own (from torch's allocator), so
-    that it may run beside any other call; it has to be kept until its work has
-    run. What is shared is the caller's to order: a Workspace that several calls
-    were given, and one prepared call itself, which one thread at a time makes, on one
-    stream.
+    that it may run beside any other call. What is shared is the caller's to order: a
+    Workspace that several calls were given, and one prepared call itself, which one thread
+    at a time makes, on one stream.
     """
 
     def __init__(self, fn, args_before_ws, workspace: Optional[Workspace], device,
@@ -302,6 +301,9 @@ class Call:
         n = ctypes.c_size_t(0)
         _check(fn(*args_before_ws, None, ctypes.byref(n), _stream()))
         self.ws = (workspace or Workspace(device)).get(n.value)
+        # streams that the allocator knows to use this call's own workspace: the one it was
+        # made on, and others once a call has run there (None: a workspace that is shared)
+        self.streams = None if workspace else {_stream().value}
         self.ws_bytes = ctypes.c_size_t(self.ws.numel())
         self.fn = fn
         self.args = tuple(args_before_ws) + (_ptr(self.ws), ctypes.byref(self.ws_bytes))
@@ -310,8 +312,20 @@ class Call:
 
     def __call__(self):
         _on_device(self.on)
-        _check(self.fn(*self.args, _stream()))
+        stream = _stream()
+        if self.streams is not None and stream.value not in self.streams and _used_here(self.ws):
+            self.streams.add(stream.value)
+        _check(self.fn(*self.args, stream))
         return self.outputs
+
+
+def _used_here(t: torch.Tensor) -> bool:
+    """Work of the current stream uses t, which its freeing has to wait for. Not while the
+    stream is captured: the replays need t, and with it the call, for as long as they run."""
+    if torch.cuda.is_current_stream_capturing():
+        return False
+    t.record_stream(torch.cuda.current_stream())
+    return True
 
 
 def prepare_lora_linear(x, W, A=None, B=None, ranks=None, adapter_idx=None, scale=None,
