@@ -80,7 +80,7 @@ struct Prefill4Args {
   int B, Hq, Hkv, group, max_blocks;
   int ranges;      // the most a tile may be split into
   int max_tiles;   // tiles that the plan has room for (of few rows: that there may be)
-  int pb;          // few rows: blocks of a partition, else 0
+  int pb;          // few rows: blocks of a partition (few_part), else 0
   float scale_log2;
   uint32_t q_xor, q_and;
 };
@@ -986,6 +986,14 @@ __device__ bool find_few(const Prefill4Args& a, int slot, FewTile* t) {
   return false;
 }
 
+// Blocks of a partition of a tile that sees so many: as in decode where the call's ranges
+// hold them, else as many times 64 as they need (the host bounds the ranges by what the
+// table's width would leave of partial results; most contexts are shorter than that).
+__device__ __forceinline__ int few_part(const Prefill4Args& a, int blocks) {
+  if (blocks <= a.ranges * a.pb) return a.pb;
+  return (blocks + kWave * a.ranges - 1) / (kWave * a.ranges) * kWave;
+}
+
 // Row r of a tile: token * Hq + query head.
 __device__ __forceinline__ int64_t few_row(const Prefill4Args& a, const FewTile& t, int g, int r) {
   const int at = t.row0 + r;
@@ -1003,10 +1011,11 @@ __global__ __launch_bounds__(kWave* W, 3) void few_kv4_kernel(Prefill4Args a) {
   const int part = rest % a.ranges;
   FewTile t;
   if (!find_few(a, rest / a.ranges, &t)) return;
-  const int n_parts = max(1, (t.blocks + a.pb - 1) / a.pb);
+  const int pb = few_part(a, t.blocks);
+  const int n_parts = max(1, (t.blocks + pb - 1) / pb);
   if (part >= n_parts) return;
   // Partitions count from the end, as in decode.
-  const int jend = t.blocks - part * a.pb, j0 = max(0, jend - a.pb);
+  const int jend = t.blocks - part * pb, j0 = max(0, jend - pb);
   const int32_t* table = a.block_table + static_cast<int64_t>(t.b) * a.max_blocks;
   const int rv = a.req_version[t.b];
   // A group of 64 blocks from jg on, a lane each: this wave's share of the valid ones.
@@ -1138,7 +1147,7 @@ template <int D>
 __global__ __launch_bounds__(kFewRows* D / 4) void few_merge_kernel(Prefill4Args a) {
   FewTile t;
   if (!find_few(a, blockIdx.x / a.Hkv, &t)) return;
-  const int n = (t.blocks + a.pb - 1) / a.pb;
+  const int pb = few_part(a, t.blocks), n = (t.blocks + pb - 1) / pb;
   if (n <= 1) return;
   const int row = threadIdx.x / (D / 4);
   if (row >= t.rows) return;
@@ -1209,21 +1218,19 @@ bool few_rows(int64_t all_rows, int B, int Hkv, int max_blocks) {
          all_rows / kFewRows + B <= kFewWork / max_blocks / Hkv;
 }
 
-// Blocks of a partition of such a call: as in decode up to kFewMost units (tile, KV head,
-// partition of a table's row), of which each may leave 16 rows of partial results, 136 MB
-// in all at D = 128; beyond, as many times 64 blocks as leave no more. (Without a bound 128
-// requests of 32 tokens with 32 heads and a 1024-block table ask for 1.1 GB.) Measured in us
-// without / with at most 16384 / 8192 / 4096 units: 128 requests of 4 tokens behind up to
-// 16000, 32/8 heads, 300 / 294 / 308 / 326; 64 of 8 behind up to 8000 142 / 147 / 144 / 154;
-// 32 of 32 behind up to 4000, 32 heads each, 165 / 154 / 150 / 124; 200 single tokens
-// behind up to 16000 373 / 374 / 415 / 386.
-constexpr int64_t kFewMost = 16384;
+// Partitions that a tile of such a call may be split into: those of the whole table while
+// they leave at most kFewPartials partial results, 136 MB at D = 128 (128 requests of 32
+// tokens with 32 heads and a 1024-block table would ask for 1.1 GB); fewer beyond. Calls
+// whose contexts are as long as their table take 0.98 to 1.00 of the time with the bound;
+// where the table is wider, workgroups without a partition go too: 64 requests of 8 tokens
+// behind up to 8000, 32/8 heads, 8192-block table, 156 us instead of 191, 100 single tokens
+// behind up to 4000 104 instead of 134. (Partitions made longer by the table's width
+// instead took those 314 and 183.)
+constexpr int64_t kFewPartials = 1 << 18;
 
-int few_part_blocks(int max_blocks, int64_t heads) {  // heads: tiles * Hkv
-  const int pb = part_blocks(max_blocks, heads);
-  if (heads * parts_of_table(max_blocks, pb) <= kFewMost) return pb;
-  const int parts = static_cast<int>(std::max<int64_t>(1, kFewMost / heads));
-  return (max_blocks + kWave * parts - 1) / (kWave * parts) * kWave;
+int few_ranges(int parts, int64_t rows) {  // rows: T * Hq
+  return static_cast<int>(
+      std::min<int64_t>(parts, std::max<int64_t>(1, kFewPartials / std::max<int64_t>(1, rows))));
 }
 
 // Key ranges that a tile of a call may be split into: as many as give every compute unit
@@ -1241,8 +1248,9 @@ int64_t tiles_of_call(Prefill4Args& a, int64_t all_rows, int B, int Hkv, int max
   const bool few = few_rows(all_rows, B, Hkv, max_blocks);
   // (B tiles more than the rows fill: each request's last one)
   const int64_t tiles = all_rows / (few ? kFewRows : kP4Rows) + B;
-  a.pb = few ? few_part_blocks(max_blocks, tiles * Hkv) : 0;
-  a.ranges = few ? parts_of_table(max_blocks, a.pb) : ranges_of_call(tiles, Hkv, max_blocks);
+  a.pb = few ? part_blocks(max_blocks, tiles * Hkv) : 0;
+  a.ranges = few ? few_ranges(parts_of_table(max_blocks, a.pb), all_rows * Hkv)
+                 : ranges_of_call(tiles, Hkv, max_blocks);
   return tiles;
 }
 
@@ -1327,12 +1335,12 @@ extern "C" local_status_t local_paged_attn_prefill_kv4(
   return D == 64 ? launch_prefill_kv4<64>(a, s) : launch_prefill_kv4<128>(a, s);
 }
 
-// What a call's size selects: 16 rows at a time, the blocks of a partition; 128 rows, minus
-// the most key ranges of a tile (for the tests, which name the form that they mean; not in
-// local.h).
+// What a call's size selects: the most key ranges of a tile, with 16 rows at a time plus 1000
+// times the blocks of a partition, with 128 rows negative (for the tests, which name the form
+// that they mean; not in local.h).
 extern "C" int32_t localk_prefill_kv4_form(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
                                            int32_t max_blocks) {
   Prefill4Args a{};
   tiles_of_call(a, T * (Hq / Hkv), B, Hkv, max_blocks);
-  return a.pb ? a.pb : -a.ranges;
+  return a.pb ? a.ranges + 1000 * a.pb : -a.ranges;
 }

@@ -41,33 +41,38 @@ def test_workspace_ceiling(D, hkv, group):
             assert n.value <= most, (B, width, T, n.value, most)
 
 
-# (prefixes, chunks, Hq, Hkv, D, table width, blocks of a partition): groups of 64 blocks
-# that begin anywhere in a partition, which count from the context's end
+# Many requests of few rows, some behind contexts of more than 64 blocks for each of the
+# ranges that the call's partial results leave: partitions of several groups of 64 blocks,
+# which count from the context's end.
+# (requests, tokens of each, first prefixes, Hq, Hkv, D, ranges)
 LONG = [
-    ([9000] + [3] * 19, [1] * 20, 8, 8, 64, 17000, 192),
-    ([3100, 2047, 5] + [30] * 29, [6, 1, 40] + [1] * 29, 8, 8, 128, 17000, 320),
-    ([1500] + [0] * 69, [2] * 70, 64, 4, 64, 17000, 896),
+    (1000, 15, [9000, 3100, 2047, 1030, 1015, 2032], 8, 8, 64, 2),
+    (4000, 2, [12000, 1023, 1024, 5000], 16, 1, 128, 2),
+    (600, 30, [4000, 995, 994, 2100, 0], 16, 16, 64, 1),
 ]
 
 
-@pytest.mark.parametrize("i", range(len(LONG)))
-def test_long_partitions_are_the_named_ones(i):
-    prefix, chunk, hq, hkv, _, width, blocks = LONG[i]
-    assert _form(sum(chunk), len(chunk), hq, hkv, width) == blocks
+def _long_prefixes(B, first):
+    return np.r_[first, np.random.default_rng(B).integers(0, 25, B - len(first))]
+
+
+@pytest.mark.parametrize("B,n,first,hq,hkv,D,ranges", LONG)
+def test_ranges_of_long_partitions(B, n, first, hq, hkv, D, ranges):
+    width = (max(first) + n + 15) // 16
+    form = _form(B * n, B, hq, hkv, width)
+    assert form > 0 and form % 1000 == ranges
+    assert width > form // 1000 * ranges
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("i", range(len(LONG)))
-def test_long_partitions(i):
+@pytest.mark.parametrize("B,n,first,hq,hkv,D,ranges", LONG)
+def test_long_partitions(B, n, first, hq, hkv, D, ranges):
     from tests.gpu_helpers import say
     from tests.kv4_cases import quick_case
-    prefix, chunk, hq, hkv, D, width, _ = LONG[i]
-    c = quick_case(300 + i, np.array(prefix) + np.array(chunk), hq, hkv, D, new=chunk, stale=0.3)
+    c = quick_case(B, _long_prefixes(B, first) + n, hq, hkv, D, new=np.full(B, n), stale=0.3)
     c.tags[c.table[0, 60:200][c.table[0, 60:200] >= 0] % c.num] -= 1  # a group wholly stale
-    c.widen()
-    assert c.table.shape[1] == width
-    say("long partitions", i, prefix[:3], chunk[:3], hq, hkv, D)
-    _run(c, range(len(chunk)))
+    say("long partitions", B, n, first, hq, hkv, D)
+    _run(c, [*range(len(first)), len(first) + 1, B - 1], append=False)
 
 
 def _check(c, b, out, lse, want, sm):
@@ -89,12 +94,12 @@ def _check(c, b, out, lse, want, sm):
         check_counts(out[rows], lse[rows], ref, ref_lse, "request %d at 0" % b)
 
 
-def _run(c, requests):
+def _run(c, requests, append=True):
     import paper_2608_15241_amd as lk
     from oracle import kv4
     from tests.gpu_helpers import dev
-    q, pool, meta, new = c.gpu()
-    tiles = c.appended()
+    q, pool, meta, new = c.gpu(append)
+    tiles = c.appended() if append else c.tiles
     want = kv4.unpack(tiles)
     for sm in (c.sm, 0.0):
         out, lse = lk.local_paged_attn_prefill_kv4(q, dev(c.starts), pool, *meta, sm, **new)
